@@ -60,6 +60,15 @@ _SIGNATURES = {
     "spr_rmsnorm_bwd": ([c_int32, c_int32, _P, _P, _P, _P, _P, _P], c_int32),
     "spr_rope_fwd": ([c_int32, c_int32, c_int32, c_int32, c_double, _P, _P, _P], c_int32),
     "spr_rope_bwd": ([c_int32, c_int32, c_int32, c_int32, c_double, _P, _P, _P], c_int32),
+    "spr_head_norm_rope_fwd": ([c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_int32, _P, c_double, _P,
+                                c_int64, _P, c_int64, _P, _P, _P, _P, _P], c_int32),
+    "spr_head_norm_rope_bwd": ([c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_int32, _P, c_double, _P,
+                                c_int64, _P, c_int64, _P, _P, _P, _P, _P, c_int64, _P, c_int64, _P, _P, c_int32, _P,
+                                c_size_t, _P], c_int32),
+    "spr_head_norm_rope_bwd_workspace_size": ([c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)], c_int32),
+    "spr_embed_fwd": ([c_int32, c_int32, c_int32, c_int32, c_float, _P, _P, _P, _P], c_int32),
+    "spr_embed_bwd": ([c_int32, c_int32, c_int32, c_int32, c_float, _P, _P, _P, _P, c_size_t, _P], c_int32),
+    "spr_embed_bwd_workspace_size": ([c_int32, c_int32, c_int32, POINTER(c_size_t)], c_int32),
     "spr_swiglu_fwd": ([c_int64, _P, _P, _P, _P], c_int32),
     "spr_swiglu_bwd": ([c_int64, _P, _P, _P, _P, _P, _P], c_int32),
     "spr_grad_accumulate": ([c_int64, _P, _P, c_int32, _P], c_int32),
@@ -403,6 +412,128 @@ def rope_bwd(dy, dx, pos0, theta, stream=None):
     t, h, d = (int(v) for v in dy.shape)
     _need_all(t * h * d, 2, dy=dy, dx=dx)
     _check(lib().spr_rope_bwd(t, h, d, pos0, float(theta), _ptr(dy), _ptr(dx), _stream(stream)))
+
+
+def _typed(dtype, **tensors):
+    """Every named tensor has elements of torch dtype ``dtype`` (fp16 has bf16's
+    size and is refused here) and lies on the current device, whose stream the
+    call takes; None is left to the library."""
+    import torch
+    for name, x in tensors.items():
+        if x is None:
+            continue
+        if x.dtype != dtype:
+            raise ValueError(f"{name}: {x.dtype}, the call needs {dtype}")
+        if x.is_cuda and x.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {x.device}, not on the current device "
+                             f"cuda:{torch.cuda.current_device()}")
+
+
+def _storage(name, x):
+    """The library's dtype code of a tensor that may be bf16 or fp32."""
+    import torch
+    code = {torch.bfloat16: SPR_BF16, torch.float32: SPR_F32}.get(x.dtype)
+    if code is None:
+        raise ValueError(f"{name}: {x.dtype}, the call takes bfloat16 or float32")
+    return code
+
+
+def _shaped(shape, **tensors):
+    for name, x in tensors.items():
+        if x is not None and tuple(x.shape) != tuple(shape):
+            raise ValueError(f"{name}: shape {tuple(x.shape)}, the call needs {tuple(shape)}")
+
+
+def _token_rows(name, x):
+    """Pointer and token stride of [tokens, heads, d] whose heads and values
+    are contiguous (a view of a fused projection)."""
+    t, h, d = (int(v) for v in x.shape)
+    if not x.is_cuda:
+        raise ValueError("libspr takes GPU tensors only")
+    if (d > 1 and x.stride(2) != 1) or (h > 1 and x.stride(1) != d):
+        raise ValueError(f"{name}: a token's heads are not contiguous")
+    stride = int(x.stride(0)) if t > 1 else h * d
+    if stride < h * d:
+        raise ValueError(f"{name}: tokens overlap (stride {stride}, a token has {h * d} elements)")
+    return x.data_ptr(), stride
+
+
+def head_norm_rope_bwd_workspace_size(tokens, q_heads, kv_heads, head_dim) -> int:
+    out = c_size_t(0)
+    _check(lib().spr_head_norm_rope_bwd_workspace_size(tokens, q_heads, kv_heads, head_dim, byref(out)))
+    return int(out.value)
+
+
+def head_norm_rope_fwd(q, k, gain_q, gain_k, yq, yk, pos0, theta, positions=None, eps=1e-6, stream=None):
+    """RMS norm of every head of q [T, Hq, d] and k [T, Hkv, d] with gains [d],
+    then the rotary embedding, in one pass; q and k may be views of one fused
+    projection (heads contiguous).  ``positions``: int32 [T], added to pos0 in
+    place of 0 .. T - 1."""
+    import torch
+    (t, hq, d), hkv = (int(v) for v in q.shape), int(k.shape[1])
+    code = _storage("q", q)
+    _typed(q.dtype, q=q, k=k, gain_q=gain_q, gain_k=gain_k, yq=yq, yk=yk)
+    _typed(torch.int32, positions=positions)
+    _shaped((t, hq, d), yq=yq)
+    _shaped((t, hkv, d), k=k, yk=yk)
+    _shaped((d,), gain_q=gain_q, gain_k=gain_k)
+    _shaped((t,), positions=positions)
+    (pq, sq), (pk, sk) = _token_rows("q", q), _token_rows("k", k)
+    _check(lib().spr_head_norm_rope_fwd(code, t, hq, hkv, d, eps, pos0, _ptr(positions), float(theta), pq, sq, pk, sk,
+                                        _ptr(gain_q), _ptr(gain_k), _ptr(yq), _ptr(yk), _stream(stream)))
+
+
+def head_norm_rope_bwd(q, k, gain_q, gain_k, dyq, dyk, dq, dk, dgain_q, dgain_k, pos0, theta, positions=None,
+                       eps=1e-6, overwrite=False, ws=None, stream=None):
+    """Backward of head_norm_rope_fwd from its inputs: dq and dk (also views of
+    one fused gradient) are written, dgain_q and dgain_k [d] fp32 added to, or
+    written where ``overwrite``."""
+    import torch
+    (t, hq, d), hkv = (int(v) for v in q.shape), int(k.shape[1])
+    code = _storage("q", q)
+    _typed(q.dtype, q=q, k=k, gain_q=gain_q, gain_k=gain_k, dyq=dyq, dyk=dyk, dq=dq, dk=dk)
+    _typed(torch.int32, positions=positions)
+    _typed(torch.float32, dgain_q=dgain_q, dgain_k=dgain_k)
+    _shaped((t, hq, d), dyq=dyq, dq=dq)
+    _shaped((t, hkv, d), k=k, dyk=dyk, dk=dk)
+    _shaped((d,), gain_q=gain_q, gain_k=gain_k, dgain_q=dgain_q, dgain_k=dgain_k)
+    _shaped((t,), positions=positions)
+    (pq, sq), (pk, sk) = _token_rows("q", q), _token_rows("k", k)
+    (pdq, sdq), (pdk, sdk) = _token_rows("dq", dq), _token_rows("dk", dk)
+    _check(lib().spr_head_norm_rope_bwd(code, t, hq, hkv, d, eps, pos0, _ptr(positions), float(theta), pq, sq, pk, sk,
+                                        _ptr(gain_q), _ptr(gain_k), _ptr(dyq), _ptr(dyk), pdq, sdq, pdk, sdk,
+                                        _ptr(dgain_q), _ptr(dgain_k), 1 if overwrite else 0, _ptr(ws), _nbytes(ws),
+                                        _stream(stream)))
+
+
+def embed_fwd(ids, table, y, scale=1.0, stream=None):
+    """y[t] = scale * table[ids[t]]; an id outside the table gives zeros."""
+    import torch
+    (t,), (v, w) = ids.shape, table.shape
+    code = _storage("table", table)
+    _typed(torch.int32, ids=ids)
+    _typed(table.dtype, table=table, y=y)
+    _shaped((t, w), y=y)
+    _check(lib().spr_embed_fwd(code, t, v, w, float(scale), _ptr(ids), _ptr(table), _ptr(y), _stream(stream)))
+
+
+def embed_bwd_workspace_size(tokens, vocab, width) -> int:
+    out = c_size_t(0)
+    _check(lib().spr_embed_bwd_workspace_size(tokens, vocab, width, byref(out)))
+    return int(out.value)
+
+
+def embed_bwd(ids, dy, dtable, scale=1.0, ws=None, stream=None):
+    """dtable[v] += scale * the sum of dy over v's tokens, fp32, in token order."""
+    import torch
+    (t,), (v, w) = ids.shape, dtable.shape
+    code = _storage("dy", dy)
+    _typed(torch.int32, ids=ids)
+    _typed(dy.dtype, dy=dy)
+    _typed(torch.float32, dtable=dtable)
+    _shaped((t, w), dy=dy)
+    _check(lib().spr_embed_bwd(code, t, v, w, float(scale), _ptr(ids), _ptr(dy), _ptr(dtable), _ptr(ws), _nbytes(ws),
+                               _stream(stream)))
 
 
 def swiglu_fwd(g, u, m, stream=None):

@@ -176,6 +176,38 @@ hipError_t launch_swiglu_bwd(long n, const void* g, const void* u, const void* d
 
 hipError_t launch_grad_accumulate(long n, const void* src, float* dst, bool overwrite, hipStream_t st);
 
+// per-head norm and rotation (kernels_heads.hip); strides in elements
+struct HeadArgs {
+  const void* q;
+  const void* k;
+  int64_t q_stride, k_stride;
+  const void* gain_q;
+  const void* gain_k;
+  void* yq;
+  void* yk;
+  const void* dyq;  // backward
+  const void* dyk;
+  void* dq;
+  void* dk;
+  int64_t dq_stride, dk_stride;
+  float* part;  // [blocks][2][d] gain-gradient partials
+  const int32_t* positions;
+  double log2_step;  // log2 of theta^(-2 / d)
+  float eps;
+  int32_t tokens, hq, hkv, d, pos0;
+};
+size_t head_norm_rope_bwd_ws(long rows, int d);
+hipError_t launch_head_norm_rope_fwd(int dtype, const HeadArgs& a, hipStream_t st);
+hipError_t launch_head_norm_rope_bwd(int dtype, const HeadArgs& a, float* dgain_q, float* dgain_k, bool overwrite,
+                                     hipStream_t st);
+
+// embedding lookup and its gradient (kernels_embed.hip)
+size_t embed_bwd_ws(long tokens, int vocab, int width);
+hipError_t launch_embed_fwd(int dtype, int tokens, int vocab, int width, float scale, const int* ids,
+                            const void* table, void* y, hipStream_t st);
+hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float scale, const int* ids, const void* dy,
+                            float* dtable, void* ws, hipStream_t st);
+
 // MoE router aux-loss accounting (kernels_moe.hip).  Statistics layout:
 // int64 count[E], double mass[E], int64 total, int64 invalid.
 int moe_blocks(int n_tokens);

@@ -1467,6 +1467,222 @@ spr_status spr_grad_accumulate(int64_t n, const void* src, float* dst, int32_t o
   return ok();
 }
 
+// ------------------------------------------- per-head norm and rotation
+namespace {
+spr_status check_dtype(int32_t dtype) {
+  if (dtype != SPR_F32 && dtype != SPR_BF16)
+    return fail(SPR_ERR_UNSUPPORTED, "dtype must be SPR_F32 or SPR_BF16");
+  return SPR_OK;
+}
+spr_status check_ws(const void* ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return SPR_OK;
+  if (ws == nullptr) return fail(SPR_ERR_WORKSPACE, "workspace is null");
+  if (ws_bytes < need)
+    return fail(SPR_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes, got " +
+                                       std::to_string(ws_bytes));
+  if (((uintptr_t)ws & 15u) != 0) return fail(SPR_ERR_MISALIGNED, "workspace is not 16-byte aligned");
+  return SPR_OK;
+}
+
+// a [tokens, heads, d] tensor whose tokens lie `stride` elements apart
+struct Rows {
+  const char* name;
+  const void* p;
+  int64_t stride;
+  size_t es, width;  // bytes of an element, elements of a token
+  int32_t tokens;
+  Buf buf() const {
+    return {p, tokens > 0 ? ((size_t)(tokens - 1) * stride + width) * es : 0, name, true, (uintptr_t)es};
+  }
+};
+// Two such tensors share no element: their ranges are apart, or their tokens
+// interleave with one stride without touching.
+bool rows_apart(const Rows& a, const Rows& b) {
+  const Buf x = a.buf(), y = b.buf();
+  if (!overlaps(x, y)) return true;
+  if (a.stride != b.stride || a.es != b.es) return false;
+  const int64_t step = a.stride * (int64_t)a.es;
+  const int64_t gap = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+  const int64_t off = ((gap % step) + step) % step;  // b's token relative to one of a's
+  return off >= (int64_t)(a.width * a.es) && off + (int64_t)(b.width * b.es) <= step;
+}
+
+spr_status check_heads(int32_t dtype, int32_t tokens, int32_t hq, int32_t hkv, int32_t d, float eps, int32_t pos0,
+                       double theta) {
+  spr_status st = check_dtype(dtype);
+  if (st != SPR_OK) return st;
+  if (hkv < 1) return fail(SPR_ERR_INVALID_ARG, "kv_heads must be >= 1");
+  if ((st = check_rope(tokens, hq, d, pos0, theta)) != SPR_OK) return st;
+  if ((int64_t)tokens * ((int64_t)hq + hkv) > INT32_MAX)
+    return fail(SPR_ERR_INVALID_ARG, "tokens * (q_heads + kv_heads) exceeds 2^31 - 1");
+  if (!(eps >= 0.f) || isinf(eps)) return fail(SPR_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  return SPR_OK;
+}
+spr_status check_strides(std::initializer_list<Rows> all) {
+  for (const Rows& r : all)
+    if (r.stride < (int64_t)r.width || r.stride > (INT64_MAX >> 34))
+      return fail(SPR_ERR_INVALID_ARG, std::string(r.name) + ": a token's stride is at least its heads' elements");
+  return SPR_OK;
+}
+HeadArgs head_args(int32_t tokens, int32_t hq, int32_t hkv, int32_t d, float eps, int32_t pos0,
+                   const int32_t* positions, double theta, const void* q, int64_t q_stride, const void* k,
+                   int64_t k_stride, const void* gain_q, const void* gain_k) {
+  HeadArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tokens = tokens;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.d = d;
+  a.eps = eps;
+  a.pos0 = pos0;
+  a.positions = positions;
+  a.log2_step = -2.0 / (double)d * log2(theta);
+  a.q = q;
+  a.q_stride = q_stride;
+  a.k = k;
+  a.k_stride = k_stride;
+  a.gain_q = gain_q;
+  a.gain_k = gain_k;
+  return a;
+}
+}  // namespace
+
+spr_status spr_head_norm_rope_fwd(int32_t dtype, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                  float eps, int32_t pos0, const int32_t* positions, double theta, const void* q,
+                                  int64_t q_stride, const void* k, int64_t k_stride, const void* gain_q,
+                                  const void* gain_k, void* yq, void* yk, hipStream_t stream) {
+  spr_status st = check_heads(dtype, tokens, q_heads, kv_heads, head_dim, eps, pos0, theta);
+  if (st != SPR_OK) return st;
+  const size_t es = dtype_bytes(dtype), wq = (size_t)q_heads * head_dim, wk = (size_t)kv_heads * head_dim;
+  const Rows rq{"q", q, q_stride, es, wq, tokens}, rk{"k", k, k_stride, es, wk, tokens};
+  if ((st = check_strides({rq, rk})) != SPR_OK) return st;
+  const std::vector<Buf> bufs = {rq.buf(), rk.buf(),
+                                 {gain_q, tokens ? head_dim * es : 0, "gain_q", true, (uintptr_t)es},
+                                 {gain_k, tokens ? head_dim * es : 0, "gain_k", true, (uintptr_t)es},
+                                 {positions, (size_t)tokens * 4, "positions", false, 4},
+                                 {yq, tokens * wq * es, "yq", true}, {yk, tokens * wk * es, "yk", true}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[5], bufs[6]}, bufs)) != SPR_OK) return st;
+  HeadArgs a = head_args(tokens, q_heads, kv_heads, head_dim, eps, pos0, positions, theta, q, q_stride, k, k_stride,
+                         gain_q, gain_k);
+  a.yq = yq;
+  a.yk = yk;
+  if ((st = hip_check(launch_head_norm_rope_fwd(dtype, a, stream), "head norm rope")) != SPR_OK) return st;
+  return ok();
+}
+
+spr_status spr_head_norm_rope_bwd_workspace_size(int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                                 size_t* bytes) {
+  spr_status st = check_heads(SPR_BF16, tokens, q_heads, kv_heads, head_dim, 0.f, 0, 2.0);
+  if (st != SPR_OK) return st;
+  if (bytes == nullptr) return fail(SPR_ERR_INVALID_ARG, "bytes is null");
+  *bytes = head_norm_rope_bwd_ws((long)tokens * (q_heads + kv_heads), head_dim);
+  return ok();
+}
+
+spr_status spr_head_norm_rope_bwd(int32_t dtype, int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                  float eps, int32_t pos0, const int32_t* positions, double theta, const void* q,
+                                  int64_t q_stride, const void* k, int64_t k_stride, const void* gain_q,
+                                  const void* gain_k, const void* dyq, const void* dyk, void* dq, int64_t dq_stride,
+                                  void* dk, int64_t dk_stride, float* dgain_q, float* dgain_k, int32_t overwrite,
+                                  void* ws, size_t ws_bytes, hipStream_t stream) {
+  spr_status st = check_heads(dtype, tokens, q_heads, kv_heads, head_dim, eps, pos0, theta);
+  if (st != SPR_OK) return st;
+  const size_t es = dtype_bytes(dtype), wq = (size_t)q_heads * head_dim, wk = (size_t)kv_heads * head_dim;
+  const Rows rq{"q", q, q_stride, es, wq, tokens}, rk{"k", k, k_stride, es, wk, tokens};
+  const Rows rdq{"dq", dq, dq_stride, es, wq, tokens}, rdk{"dk", dk, dk_stride, es, wk, tokens};
+  if ((st = check_strides({rq, rk, rdq, rdk})) != SPR_OK) return st;
+  const size_t need = head_norm_rope_bwd_ws((long)tokens * (q_heads + kv_heads), head_dim);
+  const std::vector<Buf> bufs = {rq.buf(), rk.buf(),
+                                 {gain_q, tokens ? head_dim * es : 0, "gain_q", true, (uintptr_t)es},
+                                 {gain_k, tokens ? head_dim * es : 0, "gain_k", true, (uintptr_t)es},
+                                 {positions, (size_t)tokens * 4, "positions", false, 4},
+                                 {dyq, tokens * wq * es, "dyq", true}, {dyk, tokens * wk * es, "dyk", true},
+                                 {dgain_q, (size_t)head_dim * 4, "dgain_q", true, 4},
+                                 {dgain_k, (size_t)head_dim * 4, "dgain_k", true, 4}};
+  const Buf bdq = rdq.buf(), bdk = rdk.buf(), bws{ws, need, "ws", false};
+  if ((st = check_bufs(bufs)) != SPR_OK || (st = check_bufs({bdq, bdk})) != SPR_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, need)) != SPR_OK) return st;
+  std::vector<Buf> others = bufs;
+  others.push_back(bws);
+  if ((st = check_aliasing({bufs[7], bufs[8], bws}, others)) != SPR_OK) return st;
+  if ((st = check_aliasing({bdq, bdk}, {bufs[2], bufs[3], bufs[4], bufs[5], bufs[6], bufs[7], bufs[8], bws})) != SPR_OK)
+    return st;
+  for (const Rows* out : {&rdq, &rdk})
+    for (const Rows* in : {&rq, &rk})
+      if (!rows_apart(*out, *in)) return fail(SPR_ERR_ALIASING, std::string(out->name) + " overlaps " + in->name);
+  if (!rows_apart(rdq, rdk)) return fail(SPR_ERR_ALIASING, "dq overlaps dk");
+  HeadArgs a = head_args(tokens, q_heads, kv_heads, head_dim, eps, pos0, positions, theta, q, q_stride, k, k_stride,
+                         gain_q, gain_k);
+  a.dyq = dyq;
+  a.dyk = dyk;
+  a.dq = dq;
+  a.dq_stride = dq_stride;
+  a.dk = dk;
+  a.dk_stride = dk_stride;
+  a.part = (float*)ws;
+  if ((st = hip_check(launch_head_norm_rope_bwd(dtype, a, dgain_q, dgain_k, overwrite != 0, stream),
+                      "head norm rope bwd")) != SPR_OK)
+    return st;
+  return ok();
+}
+
+// ----------------------------------------------------------- embedding
+namespace {
+spr_status check_embed(int32_t dtype, int32_t tokens, int32_t vocab, int32_t width, float scale) {
+  spr_status st = check_dtype(dtype);
+  if (st != SPR_OK) return st;
+  if (tokens < 0 || vocab < 1) return fail(SPR_ERR_INVALID_ARG, "tokens must be >= 0, vocab >= 1");
+  if (width < 8 || width % 8 != 0) return fail(SPR_ERR_UNSUPPORTED, "width must be a positive multiple of 8");
+  // one launch covers a chunk of eight values per thread, 256 a workgroup
+  if ((int64_t)tokens * (width / 8) > ((int64_t)INT32_MAX << 8))
+    return fail(SPR_ERR_INVALID_ARG, "tokens * width exceeds 2^42");
+  if (!isfinite(scale)) return fail(SPR_ERR_INVALID_ARG, "scale must be finite");
+  return SPR_OK;
+}
+}  // namespace
+
+spr_status spr_embed_fwd(int32_t dtype, int32_t tokens, int32_t vocab, int32_t width, float scale, const int32_t* ids,
+                         const void* table, void* y, hipStream_t stream) {
+  spr_status st = check_embed(dtype, tokens, vocab, width, scale);
+  if (st != SPR_OK) return st;
+  const size_t es = dtype_bytes(dtype), n = (size_t)tokens * width * es;
+  const std::vector<Buf> bufs = {{ids, (size_t)tokens * 4, "ids", true, 4},
+                                 {table, tokens ? (size_t)vocab * width * es : 0, "table", true},
+                                 {y, n, "y", true}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[2]}, bufs)) != SPR_OK) return st;
+  if ((st = hip_check(launch_embed_fwd(dtype, tokens, vocab, width, scale, ids, table, y, stream), "embed")) != SPR_OK)
+    return st;
+  return ok();
+}
+
+spr_status spr_embed_bwd_workspace_size(int32_t tokens, int32_t vocab, int32_t width, size_t* bytes) {
+  spr_status st = check_embed(SPR_F32, tokens, vocab, width, 1.f);
+  if (st != SPR_OK) return st;
+  if (bytes == nullptr) return fail(SPR_ERR_INVALID_ARG, "bytes is null");
+  *bytes = embed_bwd_ws(tokens, vocab, width);
+  return ok();
+}
+
+spr_status spr_embed_bwd(int32_t dtype, int32_t tokens, int32_t vocab, int32_t width, float scale, const int32_t* ids,
+                         const void* dy, float* dtable, void* ws, size_t ws_bytes, hipStream_t stream) {
+  spr_status st = check_embed(dtype, tokens, vocab, width, scale);
+  if (st != SPR_OK) return st;
+  const size_t need = embed_bwd_ws(tokens, vocab, width);
+  const std::vector<Buf> bufs = {{ids, (size_t)tokens * 4, "ids", true, 4},
+                                 {dy, (size_t)tokens * width * dtype_bytes(dtype), "dy", true},
+                                 {dtable, tokens ? (size_t)vocab * width * 4 : 0, "dtable", true},
+                                 {ws, need, "ws", false}};
+  if ((st = check_bufs({bufs[0], bufs[1], bufs[2]})) != SPR_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, need)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[2], bufs[3]}, bufs)) != SPR_OK) return st;
+  if ((st = hip_check(launch_embed_bwd(dtype, tokens, vocab, width, scale, ids, dy, dtable, ws, stream),
+                      "embed bwd")) != SPR_OK)
+    return st;
+  return ok();
+}
+
 // ------------------------------------------------------ MoE aux accounting
 namespace {
 spr_status check_moe(int32_t E, int32_t k) {
