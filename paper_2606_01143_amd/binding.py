@@ -72,6 +72,14 @@ _SIGNATURES = {
     "spr_swiglu_fwd": ([c_int64, _P, _P, _P, _P], c_int32),
     "spr_swiglu_bwd": ([c_int64, _P, _P, _P, _P, _P, _P], c_int32),
     "spr_grad_accumulate": ([c_int64, _P, _P, c_int32, _P], c_int32),
+    "spr_experts_plan": ([c_int32, c_int32, c_int32, _P, _P, _P, _P, _P, c_size_t, _P], c_int32),
+    "spr_experts_plan_workspace_size": ([c_int32, c_int32, c_int32, POINTER(c_size_t)], c_int32),
+    "spr_experts_fwd": ([c_int32, c_int32, c_int32, c_int32, _P, _P, c_int32, _P, _P, _P, _P, _P, _P], c_int32),
+    "spr_experts_bwd_x": ([c_int32, c_int32, c_int32, c_int32, _P, _P, _P, _P, _P, _P, _P], c_int32),
+    "spr_experts_bwd_w": ([c_int32, c_int32, c_int32, c_int32, _P, _P, c_int32, _P, _P, _P, _P, _P, c_int32, _P],
+                          c_int32),
+    "spr_experts_combine_fwd": ([c_int32, c_int32, c_int32, c_int32, _P, _P, _P, _P, _P, _P], c_int32),
+    "spr_experts_combine_bwd": ([c_int32, c_int32, c_int32, c_int32, _P, _P, _P, _P, _P, _P, _P], c_int32),
     "spr_moe_stats_bytes": ([c_int32, POINTER(c_size_t)], c_int32),
     "spr_moe_stats_zero": ([c_int32, _P, _P], c_int32),
     "spr_moe_aux_workspace_size": ([c_int32, c_int32, POINTER(c_size_t)], c_int32),
@@ -554,6 +562,106 @@ def grad_accumulate(dst, src, overwrite=False, stream=None):
     _need_all(n, 4, dst=dst)
     _need_all(n, 2, src=src)
     _check(lib().spr_grad_accumulate(n, _ptr(src), _ptr(dst), 1 if overwrite else 0, _stream(stream)))
+
+
+def experts_plan_workspace_size(n_experts, top_k, n_tokens) -> int:
+    out = c_size_t(0)
+    _check(lib().spr_experts_plan_workspace_size(n_experts, top_k, n_tokens, byref(out)))
+    return int(out.value)
+
+
+def experts_plan(n_experts, experts, offsets, row_token, pos, ws=None, stream=None):
+    """Stable sort of experts [T, k] by expert: offsets [E + 1], row_token
+    [T k] and pos [T, k], all int32; ids outside [0, E) are dropped."""
+    import torch
+    t, k = experts.shape
+    _typed(torch.int32, experts=experts, offsets=offsets, row_token=row_token, pos=pos)
+    _shaped((int(n_experts) + 1,), offsets=offsets)
+    _shaped((t * k,), row_token=row_token)
+    _shaped((t, k), pos=pos)
+    _check(lib().spr_experts_plan(n_experts, k, t, _ptr(experts), _ptr(offsets), _ptr(row_token), _ptr(pos), _ptr(ws),
+                                  _nbytes(ws), _stream(stream)))
+
+
+def experts_fwd(offsets, x, w, y, w2=None, y2=None, row_token=None, stream=None):
+    """y[r] = x[row_token[r]] w[e] (x[r] without row_token) for the rows r of
+    every expert e, w [E, in, out]; w2, y2: a second product of the same rows."""
+    import torch
+    e, i, o = w.shape
+    rows = y.shape[0]
+    _typed(torch.bfloat16, x=x, w=w, w2=w2, y=y, y2=y2)
+    _typed(torch.int32, offsets=offsets, row_token=row_token)
+    _shaped((e + 1,), offsets=offsets)
+    _shaped((rows,), row_token=row_token)
+    _shaped((x.shape[0], i), x=x)
+    _shaped((e, i, o), w2=w2)
+    _shaped((rows, o), y=y, y2=y2)
+    _check(lib().spr_experts_fwd(e, rows, i, o, _ptr(offsets), _ptr(x), x.shape[0], _ptr(row_token), _ptr(w), _ptr(y),
+                                 _ptr(w2), _ptr(y2), _stream(stream)))
+
+
+def experts_bwd_x(offsets, dy, w, dx, dy2=None, w2=None, stream=None):
+    """dx[r] = dy[r] w[e]^T (+ dy2[r] w2[e]^T) for the rows r of every expert."""
+    import torch
+    e, i, o = w.shape
+    rows = dy.shape[0]
+    _typed(torch.bfloat16, dy=dy, w=w, dx=dx, dy2=dy2, w2=w2)
+    _typed(torch.int32, offsets=offsets)
+    _shaped((e + 1,), offsets=offsets)
+    _shaped((rows, o), dy=dy, dy2=dy2)
+    _shaped((e, i, o), w2=w2)
+    _shaped((rows, i), dx=dx)
+    _check(lib().spr_experts_bwd_x(e, rows, i, o, _ptr(offsets), _ptr(dy), _ptr(w), _ptr(dy2), _ptr(w2), _ptr(dx),
+                                   _stream(stream)))
+
+
+def experts_bwd_w(offsets, x, dy, dw, dy2=None, dw2=None, row_token=None, overwrite=False, stream=None):
+    """dw[e] += the sum over e's rows of x[row_token[r]]^T dy[r], fp32 (written
+    where ``overwrite``); dy2, dw2: a second pair of the same rows."""
+    import torch
+    e, i, o = dw.shape
+    rows = dy.shape[0]
+    _typed(torch.bfloat16, x=x, dy=dy, dy2=dy2)
+    _typed(torch.float32, dw=dw, dw2=dw2)
+    _typed(torch.int32, offsets=offsets, row_token=row_token)
+    _shaped((e + 1,), offsets=offsets)
+    _shaped((rows,), row_token=row_token)
+    _shaped((x.shape[0], i), x=x)
+    _shaped((rows, o), dy=dy, dy2=dy2)
+    _shaped((e, i, o), dw2=dw2)
+    _check(lib().spr_experts_bwd_w(e, rows, i, o, _ptr(offsets), _ptr(x), x.shape[0], _ptr(row_token), _ptr(dy),
+                                   _ptr(dw), _ptr(dy2), _ptr(dw2), 1 if overwrite else 0, _stream(stream)))
+
+
+def experts_combine_fwd(y, pos, weights, out, add=None, stream=None):
+    """out[t] = add[t] + the sum over j of weights[t, j] y[pos[t, j]]; weights
+    None: ones.  A pos outside y's rows is skipped."""
+    import torch
+    t, k = pos.shape
+    rows, width = y.shape
+    _typed(torch.bfloat16, y=y, out=out, add=add)
+    _typed(torch.int32, pos=pos)
+    _typed(torch.float32, weights=weights)
+    _shaped((t, k), weights=weights)
+    _shaped((t, width), out=out, add=add)
+    _check(lib().spr_experts_combine_fwd(t, k, rows, width, _ptr(y), _ptr(pos), _ptr(weights), _ptr(add), _ptr(out),
+                                         _stream(stream)))
+
+
+def experts_combine_bwd(dout, y, pos, weights, dy, dweights, stream=None):
+    """dy[pos[t, j]] = weights[t, j] dout[t], dweights[t, j] = <y[pos[t, j]],
+    dout[t]>; y and dweights may both be None, weights None means ones."""
+    import torch
+    t, k = pos.shape
+    rows, width = dy.shape
+    _typed(torch.bfloat16, dout=dout, y=y, dy=dy)
+    _typed(torch.int32, pos=pos)
+    _typed(torch.float32, weights=weights, dweights=dweights)
+    _shaped((t, k), weights=weights, dweights=dweights)
+    _shaped((t, width), dout=dout)
+    _shaped((rows, width), y=y)
+    _check(lib().spr_experts_combine_bwd(t, k, rows, width, _ptr(dout), _ptr(y), _ptr(pos), _ptr(weights), _ptr(dy),
+                                         _ptr(dweights), _stream(stream)))
 
 
 def moe_stats_bytes(n_experts: int) -> int:

@@ -208,6 +208,31 @@ hipError_t launch_embed_fwd(int dtype, int tokens, int vocab, int width, float s
 hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float scale, const int* ids, const void* dy,
                             float* dtable, void* ws, hipStream_t st);
 
+// a router's plan and the weighted sum of the experts' rows (kernels_dispatch.hip)
+size_t experts_plan_ws(int E, long slots);
+hipError_t launch_experts_plan(int E, int k, long slots, const int* experts, int* offsets, int* row_token, int* pos,
+                               void* ws, hipStream_t st);
+hipError_t launch_combine_fwd(int tokens, int k, int rows, int width, const void* y, const int* pos,
+                              const float* weights, const void* add, void* out, hipStream_t st);
+hipError_t launch_combine_bwd(int tokens, int k, int rows, int width, const void* dout, const void* y, const int* pos,
+                              const float* weights, void* dy, float* dweights, hipStream_t st);
+
+// products grouped by expert (kernels_experts.hip)
+struct ExpertArgs {
+  const int32_t* offsets;    // [E + 1]
+  const int32_t* row_token;  // rows of `a` that the sorted rows read (fwd, bwd_w), or null
+  const void* a;             // x (fwd, bwd_w) or dy (bwd_x)
+  const void* a2;            // dy2 (bwd_x)
+  const void* b;             // w (fwd, bwd_x) or dy (bwd_w)
+  const void* b2;            // w2 or dy2; null: one product
+  void* c;                   // y, dx or dw
+  void* c2;
+  int32_t E, rows, x_rows, in_width, out_width, overwrite;
+};
+hipError_t launch_experts_fwd(const ExpertArgs& a, hipStream_t st);
+hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st);
+hipError_t launch_experts_bwd_w(const ExpertArgs& a, hipStream_t st);
+
 // MoE router aux-loss accounting (kernels_moe.hip).  Statistics layout:
 // int64 count[E], double mass[E], int64 total, int64 invalid.
 int moe_blocks(int n_tokens);

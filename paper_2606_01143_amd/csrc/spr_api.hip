@@ -15,6 +15,7 @@
 #include "../../include/spr.h"
 #include "../../include/spr_moe.h"
 #include "../../include/spr_layer.h"
+#include "../../include/spr_experts.h"
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -1679,6 +1680,208 @@ spr_status spr_embed_bwd(int32_t dtype, int32_t tokens, int32_t vocab, int32_t w
   if ((st = check_aliasing({bufs[2], bufs[3]}, bufs)) != SPR_OK) return st;
   if ((st = hip_check(launch_embed_bwd(dtype, tokens, vocab, width, scale, ids, dy, dtable, ws, stream),
                       "embed bwd")) != SPR_OK)
+    return st;
+  return ok();
+}
+
+// ------------------------------------------------------------ experts
+namespace {
+spr_status check_experts(int32_t E) {
+  if (E < 1 || E > 1024) return fail(SPR_ERR_UNSUPPORTED, "n_experts must be in [1, 1024]");
+  return SPR_OK;
+}
+spr_status check_slots(int32_t tokens, int32_t k) {
+  if (tokens < 0) return fail(SPR_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (k < 1) return fail(SPR_ERR_INVALID_ARG, "top_k must be >= 1");
+  if ((int64_t)tokens * k > INT32_MAX) return fail(SPR_ERR_INVALID_ARG, "n_tokens * top_k exceeds 2^31 - 1");
+  return SPR_OK;
+}
+spr_status check_plan(int32_t E, int32_t k, int32_t tokens) {
+  spr_status st = check_experts(E);
+  if (st != SPR_OK) return st;
+  if ((st = check_slots(tokens, k)) != SPR_OK) return st;
+  if (k > E) return fail(SPR_ERR_INVALID_ARG, "top_k must be at most n_experts");
+  return SPR_OK;
+}
+spr_status check_width(const char* name, int32_t w) {
+  if (w < 8 || w % 8 != 0) return fail(SPR_ERR_UNSUPPORTED, std::string(name) + " must be a positive multiple of 8");
+  return SPR_OK;
+}
+spr_status check_products(int32_t E, int32_t rows, int32_t in_width, int32_t out_width, bool gathers, int32_t x_rows) {
+  spr_status st = check_experts(E);
+  if (st != SPR_OK) return st;
+  if (rows < 0) return fail(SPR_ERR_INVALID_ARG, "rows must be >= 0");
+  if ((st = check_width("in_width", in_width)) != SPR_OK) return st;
+  if ((st = check_width("out_width", out_width)) != SPR_OK) return st;
+  if (rows > 0 && x_rows < (gathers ? 1 : rows))
+    return fail(SPR_ERR_INVALID_ARG, gathers ? "x_rows must be >= 1" : "x_rows must be >= rows without row_token");
+  // the launch's tiles: 32 rows and 32 columns each at the least
+  if (((int64_t)rows / 32 + E) * (2 * ((int64_t)(in_width > out_width ? in_width : out_width) / 32 + 1)) > INT32_MAX ||
+      (int64_t)E * 2 * (in_width / 32 + 1) * (out_width / 32 + 1) > INT32_MAX)
+    return fail(SPR_ERR_INVALID_ARG, "rows and widths need more than 2^31 - 1 tiles");
+  return SPR_OK;
+}
+spr_status check_pair(const char* what, const void* a, const void* b) {
+  if ((a == nullptr) != (b == nullptr)) return fail(SPR_ERR_INVALID_ARG, std::string(what) + " go together");
+  return SPR_OK;
+}
+ExpertArgs expert_args(int32_t E, int32_t rows, int32_t in_width, int32_t out_width, const int32_t* offsets) {
+  ExpertArgs a;
+  memset(&a, 0, sizeof(a));
+  a.E = E;
+  a.rows = rows;
+  a.in_width = in_width;
+  a.out_width = out_width;
+  a.offsets = offsets;
+  return a;
+}
+}  // namespace
+
+spr_status spr_experts_plan_workspace_size(int32_t n_experts, int32_t top_k, int32_t n_tokens, size_t* bytes) {
+  spr_status st = check_plan(n_experts, top_k, n_tokens);
+  if (st != SPR_OK) return st;
+  if (bytes == nullptr) return fail(SPR_ERR_INVALID_ARG, "bytes is null");
+  *bytes = experts_plan_ws(n_experts, (long)n_tokens * top_k);
+  return ok();
+}
+
+spr_status spr_experts_plan(int32_t n_experts, int32_t top_k, int32_t n_tokens, const int32_t* experts,
+                            int32_t* offsets, int32_t* row_token, int32_t* pos, void* ws, size_t ws_bytes,
+                            hipStream_t stream) {
+  spr_status st = check_plan(n_experts, top_k, n_tokens);
+  if (st != SPR_OK) return st;
+  const size_t n = (size_t)n_tokens * top_k, need = experts_plan_ws(n_experts, (long)n);
+  const std::vector<Buf> bufs = {{experts, n * 4, "experts", true, 4},
+                                 {offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
+                                 {row_token, n * 4, "row_token", true, 4},
+                                 {pos, n * 4, "pos", true, 4},
+                                 {ws, need, "ws", false}};
+  if ((st = check_bufs({bufs[0], bufs[1], bufs[2], bufs[3]})) != SPR_OK) return st;
+  if ((st = check_ws(ws, ws_bytes, need)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[1], bufs[2], bufs[3], bufs[4]}, bufs)) != SPR_OK) return st;
+  if ((st = hip_check(launch_experts_plan(n_experts, top_k, (long)n, experts, offsets, row_token, pos, ws, stream),
+                      "experts plan")) != SPR_OK)
+    return st;
+  return ok();
+}
+
+spr_status spr_experts_fwd(int32_t n_experts, int32_t rows, int32_t in_width, int32_t out_width,
+                           const int32_t* offsets, const void* x, int32_t x_rows, const int32_t* row_token,
+                           const void* w, void* y, const void* w2, void* y2, hipStream_t stream) {
+  spr_status st = check_products(n_experts, rows, in_width, out_width, row_token != nullptr, x_rows);
+  if (st != SPR_OK) return st;
+  if ((st = check_pair("w2 and y2", w2, y2)) != SPR_OK) return st;
+  if (rows == 0) return ok();
+  const size_t wb = (size_t)n_experts * in_width * out_width * 2, yb = (size_t)rows * out_width * 2;
+  const std::vector<Buf> bufs = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
+                                 {x, (size_t)x_rows * in_width * 2, "x", true},
+                                 {row_token, (size_t)rows * 4, "row_token", false, 4},
+                                 {w, wb, "w", true}, {w2, wb, "w2", false},
+                                 {y, yb, "y", true}, {y2, yb, "y2", false}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[5], bufs[6]}, bufs)) != SPR_OK) return st;
+  ExpertArgs a = expert_args(n_experts, rows, in_width, out_width, offsets);
+  a.a = x;
+  a.x_rows = x_rows;
+  a.row_token = row_token;
+  a.b = w;
+  a.b2 = w2;
+  a.c = y;
+  a.c2 = y2;
+  if ((st = hip_check(launch_experts_fwd(a, stream), "experts fwd")) != SPR_OK) return st;
+  return ok();
+}
+
+spr_status spr_experts_bwd_x(int32_t n_experts, int32_t rows, int32_t in_width, int32_t out_width,
+                             const int32_t* offsets, const void* dy, const void* w, const void* dy2, const void* w2,
+                             void* dx, hipStream_t stream) {
+  spr_status st = check_products(n_experts, rows, in_width, out_width, false, rows);
+  if (st != SPR_OK) return st;
+  if ((st = check_pair("dy2 and w2", dy2, w2)) != SPR_OK) return st;
+  if (rows == 0) return ok();
+  const size_t wb = (size_t)n_experts * in_width * out_width * 2, yb = (size_t)rows * out_width * 2;
+  const std::vector<Buf> bufs = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
+                                 {dy, yb, "dy", true}, {w, wb, "w", true}, {dy2, yb, "dy2", false},
+                                 {w2, wb, "w2", false}, {dx, (size_t)rows * in_width * 2, "dx", true}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[5]}, bufs)) != SPR_OK) return st;
+  ExpertArgs a = expert_args(n_experts, rows, in_width, out_width, offsets);
+  a.a = dy;
+  a.a2 = dy2;
+  a.b = w;
+  a.b2 = w2;
+  a.c = dx;
+  if ((st = hip_check(launch_experts_bwd_x(a, stream), "experts bwd x")) != SPR_OK) return st;
+  return ok();
+}
+
+spr_status spr_experts_bwd_w(int32_t n_experts, int32_t rows, int32_t in_width, int32_t out_width,
+                             const int32_t* offsets, const void* x, int32_t x_rows, const int32_t* row_token,
+                             const void* dy, float* dw, const void* dy2, float* dw2, int32_t overwrite,
+                             hipStream_t stream) {
+  spr_status st = check_products(n_experts, rows, in_width, out_width, row_token != nullptr, x_rows);
+  if (st != SPR_OK) return st;
+  if ((st = check_pair("dy2 and dw2", dy2, dw2)) != SPR_OK) return st;
+  if (rows == 0 && overwrite == 0) return ok();
+  const size_t wb = (size_t)n_experts * in_width * out_width * 4, yb = (size_t)rows * out_width * 2;
+  const std::vector<Buf> bufs = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
+                                 {x, rows ? (size_t)x_rows * in_width * 2 : 0, "x", true},
+                                 {row_token, (size_t)rows * 4, "row_token", false, 4},
+                                 {dy, yb, "dy", true}, {dy2, yb, "dy2", false},
+                                 {dw, wb, "dw", true}, {dw2, wb, "dw2", false}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[5], bufs[6]}, bufs)) != SPR_OK) return st;
+  ExpertArgs a = expert_args(n_experts, rows, in_width, out_width, offsets);
+  a.a = x;
+  a.x_rows = x_rows;
+  a.row_token = row_token;
+  a.b = dy;
+  a.b2 = dy2;
+  a.c = dw;
+  a.c2 = dw2;
+  a.overwrite = overwrite != 0;
+  if ((st = hip_check(launch_experts_bwd_w(a, stream), "experts bwd w")) != SPR_OK) return st;
+  return ok();
+}
+
+spr_status spr_experts_combine_fwd(int32_t n_tokens, int32_t top_k, int32_t rows, int32_t width, const void* y,
+                                   const int32_t* pos, const float* weights, const void* add, void* out,
+                                   hipStream_t stream) {
+  spr_status st = check_slots(n_tokens, top_k);
+  if (st != SPR_OK) return st;
+  if (rows < 0) return fail(SPR_ERR_INVALID_ARG, "rows must be >= 0");
+  if ((st = check_width("width", width)) != SPR_OK) return st;
+  const size_t n = (size_t)n_tokens, tb = n * width * 2;
+  const std::vector<Buf> bufs = {{y, n ? (size_t)rows * width * 2 : 0, "y", true},
+                                 {pos, n * top_k * 4, "pos", true, 4},
+                                 {weights, n * top_k * 4, "weights", false, 4},
+                                 {add, tb, "add", false}, {out, tb, "out", true}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[4]}, {bufs[0], bufs[1], bufs[2]})) != SPR_OK) return st;
+  if (add != out && (st = check_aliasing({bufs[4]}, {bufs[3]})) != SPR_OK) return st;
+  if ((st = hip_check(launch_combine_fwd(n_tokens, top_k, rows, width, y, pos, weights, add, out, stream),
+                      "experts combine")) != SPR_OK)
+    return st;
+  return ok();
+}
+
+spr_status spr_experts_combine_bwd(int32_t n_tokens, int32_t top_k, int32_t rows, int32_t width, const void* dout,
+                                   const void* y, const int32_t* pos, const float* weights, void* dy,
+                                   float* dweights, hipStream_t stream) {
+  spr_status st = check_slots(n_tokens, top_k);
+  if (st != SPR_OK) return st;
+  if (rows < 0) return fail(SPR_ERR_INVALID_ARG, "rows must be >= 0");
+  if ((st = check_width("width", width)) != SPR_OK) return st;
+  const size_t n = (size_t)n_tokens, rb = n ? (size_t)rows * width * 2 : 0;
+  if (rb > 0 && (st = check_pair("y and dweights", y, dweights)) != SPR_OK) return st;
+  const std::vector<Buf> bufs = {{dout, n * width * 2, "dout", true}, {y, rb, "y", false},
+                                 {pos, n * top_k * 4, "pos", true, 4},
+                                 {weights, n * top_k * 4, "weights", false, 4},
+                                 {dy, rb, "dy", true}, {dweights, n * top_k * 4, "dweights", false, 4}};
+  if ((st = check_bufs(bufs)) != SPR_OK) return st;
+  if ((st = check_aliasing({bufs[4], bufs[5]}, bufs)) != SPR_OK) return st;
+  if ((st = hip_check(launch_combine_bwd(n_tokens, top_k, rows, width, dout, y, pos, weights, dy, dweights, stream),
+                      "experts combine bwd")) != SPR_OK)
     return st;
   return ok();
 }
