@@ -17,6 +17,9 @@
 // (both operands: a zero times another row's infinity would be a NaN); C rows
 // and columns past the end repeat a valid address and are not stored.  A wave
 // whose rows are all past the end skips its products.
+#include <type_traits>
+#include <utility>
+
 #include "launch.hpp"
 #include "tile.hpp"
 
@@ -24,10 +27,13 @@ namespace spr {
 
 namespace {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 enum ExpertMode { kFwd = 0, kBwdX = 1, kBwdW = 2 };
 constexpr int kStep = 32;   // contraction indices per step
 constexpr int kRing = 3;    // tile buffers
 constexpr int kXcds = 8;
+constexpr int kBand = 4;    // tile rows of a band
 
 __device__ const uint4 zero_line = {0, 0, 0, 0};
 
@@ -48,15 +54,19 @@ struct Natural {
 #pragma unroll
     for (int i = 0; i < I; ++i) p[i] = (const char*)(row_ptr(16 * ((w + WAVES * i) % N) + (lane >> 2)) + col);
   }
-  // indices k0 .. k0 + 31 of [.., end), `off` bytes from each row's pointer
-  __device__ __forceinline__ void load(bf16* tile, long off, int k0, int end) const {
-    const bool cut = k0 + kStep > end;
+  __device__ __forceinline__ void advance(long bytes) {
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const char* q = p[i] + off;
-      if (cut) q = k0 + col < end ? q : (const char*)&zero_line;
-      dma_lds16(q, lds_addr(tile + 512 * ((w + WAVES * i) % N)));
-    }
+    for (int i = 0; i < I; ++i) p[i] += bytes;
+  }
+  // chunks of a step with `left` indices that are past the end
+  __device__ __forceinline__ void stop(int left) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) p[i] = col < left ? p[i] : (const char*)&zero_line;
+  }
+  // load i of the step the pointers stand at
+  template <int i>
+  __device__ __forceinline__ void load(bf16* tile) const {
+    dma_lds16(p[i], lds_addr(tile + 512 * ((w + WAVES * i) % N)));
   }
   static __device__ __forceinline__ int frag(int lane, int v) {
     const int r = lane & 31, h = lane >> 5;
@@ -68,30 +78,34 @@ struct Natural {
 template <int COLS, int WAVES>
 struct Transposed {
   static constexpr int N = COLS / 16, I = (N + WAVES - 1) / WAVES;
-  int row[I], col[I], w;
-  __device__ __forceinline__ void init(int wave, int lane, int ncols) {
+  const char* p[I];  // column of load i in row 0 of `base`
+  int row[I], w;
+  __device__ __forceinline__ void init(int wave, int lane, const bf16* base, int ncols) {
     w = wave;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const int q = (w + WAVES * i) % N;  // panel q / 8, rows 4 (q % 8) ..
       row[i] = 4 * (q & 7) + (lane >> 4);
       const int c = 128 * (q >> 3) + 8 * ((lane & 15) ^ swz<128>(row[i]));
-      col[i] = c < ncols ? c : 0;
+      p[i] = (const char*)(base + (c < ncols ? c : 0));
     }
   }
-  // row_ptr(k): contraction row k's first column of this tile
-  template <typename RowPtr>
-  __device__ __forceinline__ void load(bf16* tile, int k0, int end, RowPtr row_ptr) const {
-    const bool cut = k0 + kStep > end;
+  // rows `ld` bytes apart: the pointers move to their load's own row
+  __device__ __forceinline__ void own_rows(long ld) {
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      const bf16* q;
-      if (cut)
-        q = k0 + row[i] < end ? row_ptr(k0 + row[i]) + col[i] : (const bf16*)&zero_line;
-      else
-        q = row_ptr(k0 + row[i]) + col[i];
-      dma_lds16(q, lds_addr(tile + 512 * ((w + WAVES * i) % N)));
-    }
+    for (int i = 0; i < I; ++i) p[i] += row[i] * ld;
+  }
+  __device__ __forceinline__ void advance(long bytes) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) p[i] += bytes;
+  }
+  __device__ __forceinline__ void stop(int left) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) p[i] = row[i] < left ? p[i] : (const char*)&zero_line;
+  }
+  template <int i>
+  __device__ __forceinline__ void load(bf16* tile, unsigned long extra = 0) const {
+    dma_lds16(p[i] + extra, lds_addr(tile + 512 * ((w + WAVES * i) % N)));
   }
   // element offset of 32-column block b's operand, contraction rows 8 h + 4 hi ..
   static __device__ __forceinline__ int frag(int lane, int b, int hi) {
@@ -107,6 +121,41 @@ __device__ __forceinline__ bf16x8 tr_pair(const bf16* lo, const bf16* hi) {
   return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
+// The tokens of the contraction rows that one wave loads in a step: rows 4 w ..
+// and 16 + 4 w .. (rows past the end: token 0, which adds nothing to the address
+// of the line of zeros).  Scalar loads one step ahead of their use: a vector
+// load's wait would also wait for the tiles in flight.
+template <int WAVES>
+struct StepTokens {
+  static_assert(WAVES == 4, "a wave's loads cover two groups of four rows");
+  i32x4 lo4, hi4;  // vectors, not arrays: those would be moved to LDS
+  __device__ __forceinline__ void fetch(const int32_t* row_token, int lo, int k0, int len, int w) {
+    typedef const __attribute__((address_space(4))) int32_t scalar_int;
+    scalar_int* src = (scalar_int*)(uintptr_t)(row_token + lo);
+    const int k = k0 + 4 * w;
+    auto at = [&](int q) { return k + q < len ? src[k + q] : 0; };
+    lo4 = i32x4{at(0), at(1), at(2), at(3)};
+    hi4 = i32x4{at(16), at(17), at(18), at(19)};
+  }
+  // of load i, this lane's row
+  __device__ __forceinline__ int of(int i, int lane) const {
+    const i32x4 v = i & 1 ? hi4 : lo4;
+    const int a = lane & 16 ? v[1] : v[0], b = lane & 16 ? v[3] : v[2];
+    return lane & 32 ? b : a;
+  }
+};
+
+// f(0), f(1), .. f(N - 1) with each index a compile-time constant: register
+// arrays are then never indexed by a variable
+template <typename F, int... J>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, J...>, F f) {
+  (f(std::integral_constant<int, J>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
+
 template <int N>
 __device__ __forceinline__ void wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(N) : "memory");
@@ -118,8 +167,10 @@ struct GroupTile {
   bool any;
 };
 
-// Tile t of the launch: experts in order, each expert's tiles column by
-// column (`cols` columns of tiles), ceil(len / BM) rows of tiles.  A wave adds
+// Tile t of the launch: experts in order, each expert's ceil(len / BM) rows of
+// tiles in bands of kBand rows, a band column by column (`cols` columns).  The
+// 64 workgroups that an XCD runs at once then share kBand tiles of rows and
+// most columns of the weights.  A wave adds
 // up the experts' tile rows 64 ranges at a time and finds the one that holds t.
 // The workgroups of one XCD (blockIdx modulo 8) take consecutive tiles, which
 // share an expert's weights and rows in its L2.
@@ -156,8 +207,10 @@ __device__ __forceinline__ GroupTile find_tile(const ExpertArgs& a, int cols, in
     g.len = rows_of(g.e, g.lo);
     const int mt = (g.len + BM - 1) / BM;
     if (left >= 0 && left < (long)mt * cols) {
-      g.m0 = (int)(left % mt) * BM;
-      g.n0 = (int)(left / mt);  // column of tiles; the caller turns it into columns
+      const int band = (int)(left / (kBand * cols)), in = (int)(left % (kBand * cols));
+      const int high = min(kBand, mt - band * kBand);
+      g.m0 = (band * kBand + in % high) * BM;
+      g.n0 = in / high;  // column of tiles; the caller turns it into columns
       return g;
     }
     left -= (long)mt * cols;
@@ -173,7 +226,7 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   constexpr int A_ELEMS = BM * kStep, B_ELEMS = BN * kStep;
   constexpr int LOADS = (BM / 16 + WAVES - 1) / WAVES + (BN / 16 + WAVES - 1) / WAVES;
   constexpr int OUT_STRIDE = NI * 32 + 8;  // staged output rows, 16 bytes apart in banks
-  constexpr int SMEM = kRing * (A_ELEMS + B_ELEMS);
+  constexpr int STAGE = A_ELEMS + B_ELEMS, SMEM = kRing * STAGE;  // elements
   static_assert(WAVES * 32 * OUT_STRIDE <= SMEM, "the output staging fits the ring");
   __shared__ __attribute__((aligned(1024))) bf16 smem[SMEM];
   const int lane = threadIdx.x & 63, w = wave_id(), wm = w / NW, wn = w % NW;
@@ -210,68 +263,110 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   const int steps = MODE == kBwdX ? steps1 * parts : steps1;
   const size_t wsize = (size_t)a.in_width * a.out_width;
 
+  const bool gathers = MODE != kBwdX && a.row_token != nullptr;
+
   // ---- operands
-  const bf16* bsrc = g.part != 0 && MODE != kBwdX ? (const bf16*)a.b2 : (const bf16*)a.b;
   Natural<BM, WAVES> an;
   Transposed<BM, WAVES> at;
   Natural<BN, WAVES> bn;
   Transposed<BN, WAVES> bt;
-  long a_part = 0, b_part = 0;  // bytes from a pair's first operands to its second's
-  if constexpr (!A_TR) {
-    an.init(w, lane, [&](int m) {
-      const int row = g.lo + g.m0 + min(m, mrows - 1);
-      long src = row;
-      if (MODE == kFwd && a.row_token != nullptr) src = clampi(a.row_token[row], 0, a.x_rows - 1);
-      return (const bf16*)a.a + src * depth;
-    });
-    if (MODE == kBwdX && parts == 2) a_part = (const char*)a.a2 - (const char*)a.a;
-  } else {
-    at.init(w, lane, mrows);
-  }
-  if constexpr (!B_TR) {
-    bn.init(w, lane, [&](int n) {
-      return bsrc + g.e * wsize + (size_t)min(g.n0 + n, ncols - 1) * a.out_width;
-    });
-    if (parts == 2) b_part = (const char*)a.b2 - (const char*)a.b;
-  } else {
-    bt.init(w, lane, ncols - g.n0);
-  }
-  auto issue = [&](int s) {
-    bf16* ta = smem + (s % kRing) * (A_ELEMS + B_ELEMS);
-    bf16* tb = ta + A_ELEMS;
-    const bool second = MODE == kBwdX && s >= steps1;
-    const int k0 = (second ? s - steps1 : s) * kStep;
-    if constexpr (!A_TR)
-      an.load(ta, 2L * k0 + (second ? a_part : 0), k0, depth);
-    else
-      at.load(ta, k0, depth, [&](int k) {
-        long src = g.lo + k;
-        if (a.row_token != nullptr) src = clampi(a.row_token[src], 0, a.x_rows - 1);
-        return (const bf16*)a.a + src * a.in_width + g.m0;
+  // pointers at the first step of a part
+  auto start = [&](int part) {
+    if constexpr (!A_TR) {
+      an.init(w, lane, [&](int m) {
+        const int row = g.lo + g.m0 + min(m, mrows - 1);
+        long src = row;
+        if (gathers) src = clampi(a.row_token[row], 0, a.x_rows - 1);
+        return (const bf16*)(part ? a.a2 : a.a) + src * depth;
       });
-    if constexpr (!B_TR)
-      bn.load(tb, 2L * k0 + (second ? b_part : 0), k0, depth);
-    else if constexpr (MODE == kFwd)
-      bt.load(tb, k0, depth, [&](int k) { return bsrc + g.e * wsize + (size_t)k * a.out_width + g.n0; });
+    } else {
+      at.init(w, lane, (const bf16*)a.a + g.m0 + (gathers ? 0 : (size_t)g.lo * a.in_width), mrows);
+      if (!gathers) at.own_rows(2L * a.in_width);
+    }
+    if constexpr (!B_TR) {
+      bn.init(w, lane, [&](int n) {
+        return (const bf16*)(part ? a.b2 : a.b) + g.e * wsize + (size_t)min(g.n0 + n, ncols - 1) * a.out_width;
+      });
+    } else {
+      const size_t row0 = MODE == kFwd ? (size_t)g.e * a.in_width : (size_t)g.lo;
+      bt.init(w, lane, (const bf16*)(g.part ? a.b2 : a.b) + row0 * a.out_width + g.n0, ncols - g.n0);
+      bt.own_rows(2L * a.out_width);
+    }
+  };
+  start(0);
+  StepTokens<A_TR ? WAVES : 4> tok;
+  if constexpr (A_TR)
+    if (gathers && steps > 0) tok.fetch(a.row_token, g.lo, 0, g.len, w);
+  // The pointers stand at the next step to issue; tok holds its tokens.
+  constexpr int IA = (BM / 16 + WAVES - 1) / WAVES, IB = (BN / 16 + WAVES - 1) / WAVES;
+  const long a_step = A_TR ? 2L * kStep * a.in_width : 2L * kStep;
+  const long b_step = B_TR ? 2L * kStep * a.out_width : 2L * kStep;
+  auto gathered = [&](int i) -> unsigned long {  // bytes to the row of load i's token
+    if (!A_TR || !gathers) return 0;
+    return (unsigned long)(unsigned)clampi(tok.of(i, lane), 0, a.x_rows - 1) * (2u * a.in_width);
+  };
+  // load j of the LOADS of a step into buffer `buf` (elements into the ring)
+  auto load = [&](auto index, int buf) {
+    constexpr int j = decltype(index)::value;
+    if constexpr (j < IA) {
+      if constexpr (A_TR)
+        at.template load<j>(smem + buf, gathered(j));
+      else
+        an.template load<j>(smem + buf);
+    } else {
+      if constexpr (B_TR)
+        bt.template load<j - IA>(smem + buf + A_ELEMS);
+      else
+        bn.template load<j - IA>(smem + buf + A_ELEMS);
+    }
+  };
+  // Points the loads at step s, whose predecessor they stood at.  Past the last
+  // index they read zeros: the last step of a part that is not whole, and the
+  // steps behind the last one, which the loop issues like all others.
+  auto aim = [&](int s) {
+    const bool second = MODE == kBwdX && s >= steps1;
+    const int left = s < steps ? depth - (second ? s - steps1 : s) * kStep : 0;
+    if (MODE == kBwdX && s == steps1 && s < steps) start(1);
+    if (left < kStep) {
+      if constexpr (A_TR)
+        at.stop(left);
+      else
+        an.stop(left);
+      if constexpr (B_TR)
+        bt.stop(left);
+      else
+        bn.stop(left);
+    }
+  };
+  auto advance = [&](int s) {
+    if constexpr (!A_TR)
+      an.advance(a_step);
+    else if (!gathers)
+      at.advance(a_step);
     else
-      bt.load(tb, k0, depth, [&](int k) { return bsrc + (size_t)(g.lo + k) * a.out_width + g.n0; });
+      tok.fetch(a.row_token, g.lo, s * kStep, g.len, w);
+    if constexpr (!B_TR)
+      bn.advance(b_step);
+    else
+      bt.advance(b_step);
+    aim(s);
   };
 
-  // ---- offsets of the operand reads
+  // ---- byte offsets of the operand reads
   int aoff[2][A_TR ? MI : 1], boff[2][B_TR ? NI : 1];
 #pragma unroll
   for (int v = 0; v < 2; ++v) {
     if constexpr (A_TR) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) aoff[v][i] = Transposed<BM, WAVES>::frag(lane, i * MW + wm, v);
+      for (int i = 0; i < MI; ++i) aoff[v][i] = 2 * Transposed<BM, WAVES>::frag(lane, i * MW + wm, v);
     } else {
-      aoff[v][0] = Natural<BM, WAVES>::frag(lane, v) + wm * 32 * kStep;
+      aoff[v][0] = 2 * (Natural<BM, WAVES>::frag(lane, v) + wm * 32 * kStep);
     }
     if constexpr (B_TR) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) boff[v][i] = Transposed<BN, WAVES>::frag(lane, wn * NI + i, v);
+      for (int i = 0; i < NI; ++i) boff[v][i] = 2 * Transposed<BN, WAVES>::frag(lane, wn * NI + i, v);
     } else {
-      boff[v][0] = Natural<BN, WAVES>::frag(lane, v) + wn * NI * 32 * kStep;
+      boff[v][0] = 2 * (Natural<BN, WAVES>::frag(lane, v) + wn * NI * 32 * kStep);
     }
   }
 
@@ -281,42 +376,84 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
 #pragma unroll
     for (int m = 0; m < MI; ++m) acc[n][m] = zero16();
 
-  for (int s = 0; s < min(kRing - 1, steps); ++s) issue(s);
-  for (int s = 0; s < steps; ++s) {
-    if (s + 1 < steps)
-      wait_barrier<LOADS>();
-    else
-      wait_barrier<0>();
-    if (s + kRing - 1 < steps) issue(s + kRing - 1);
-    const bf16* ta = smem + (s % kRing) * (A_ELEMS + B_ELEMS);
-    const bf16* tb = ta + A_ELEMS;
-    if (act == 0) continue;
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      bf16x8 fb[NI], fa[MI];
-#pragma unroll
-      for (int n = 0; n < NI; ++n) {
+  // One half step (16 contraction indices) of operands is read ahead of the
+  // products.  The barrier stands between a step's halves: by then every wave
+  // has read the whole step, so its buffer takes step s + 3 at once, and the
+  // next step, whose loads are waited for there, is read while the second
+  // half's products run.
+  if (steps > 0) {
+    aim(0);
+    each<kRing>([&](auto s) {
+      each<LOADS>([&](auto j) { load(j, s * STAGE); });
+      advance(s + 1);
+    });
+  }
+  auto sweep = [&](auto active) {
+    constexpr int ACT = decltype(active)::value;
+    bf16x8 fb[2][NI], fa[2][ACT > 0 ? ACT : 1];
+    constexpr int FRAGS = ACT > 0 ? ACT + NI : 0, PRODUCTS = ACT * NI;
+    constexpr int MOST = PRODUCTS > FRAGS ? PRODUCTS : FRAGS, MOST2 = MOST > LOADS ? MOST : LOADS;
+    // fragment j of half v, in the order of use: b0 a0 b1 .. then the other a
+    auto read = [&](int buf, auto half, auto index) {
+      constexpr int v = decltype(half)::value, j = decltype(index)::value;
+      const char* ta = (const char*)smem + 2 * buf;
+      const char* tb = ta + 2 * A_ELEMS;
+      if constexpr (j != 1 && j <= NI) {
+        constexpr int n = j == 0 ? 0 : j - 1;
         if constexpr (B_TR)
-          fb[n] = tr_pair(tb + boff[0][n] + v * 16 * 128, tb + boff[1][n] + v * 16 * 128);
+          fb[v][n] = tr_pair((const bf16*)(tb + boff[0][n]) + v * 16 * 128, (const bf16*)(tb + boff[1][n]) + v * 16 * 128);
         else
-          fb[n] = *(const bf16x8*)(tb + boff[v][0] + n * 32 * kStep);
-      }
-#pragma unroll
-      for (int m = 0; m < MI; ++m) {
+          fb[v][n] = *((const bf16x8*)(tb + boff[v][0]) + n * 4 * kStep);
+      } else {
+        constexpr int m = j == 1 ? 0 : j - NI;
         if constexpr (A_TR)
-          fa[m] = tr_pair(ta + aoff[0][m] + v * 16 * 128, ta + aoff[1][m] + v * 16 * 128);
+          fa[v][m] = tr_pair((const bf16*)(ta + aoff[0][m]) + v * 16 * 128, (const bf16*)(ta + aoff[1][m]) + v * 16 * 128);
         else
-          fa[m] = *(const bf16x8*)(ta + aoff[v][0] + m * MW * 32 * kStep);
+          fa[v][m] = *((const bf16x8*)(ta + aoff[v][0]) + m * MW * 4 * kStep);
       }
-#pragma unroll
-      for (int n = 0; n < NI; ++n)
-#pragma unroll
-        for (int m = 0; m < MI; ++m) acc[n][m] = mfma32(fb[n], fa[m], acc[n][m]);
+    };
+    auto multiply = [&](auto half, auto index) {
+      constexpr int v = decltype(half)::value, m = decltype(index)::value / NI, n = decltype(index)::value % NI;
+      acc[n][m] = mfma32(fb[v][n], fa[v][m], acc[n][m]);
+    };
+    const std::integral_constant<int, 0> first{};
+    const std::integral_constant<int, 1> second{};
+    if (steps == 0) return;
+    wait_barrier<(kRing - 1) * LOADS>();
+    each<FRAGS>([&](auto j) { read(0, first, j); });
+    int buf = 0;
+    for (int s = 0; s < steps; ++s) {
+      asm volatile("" : "+s"(buf));  // one scalar offset, not a register per address
+      const int next = buf + STAGE < kRing * STAGE ? buf + STAGE : 0;
+      // each product is followed by a read of the other half
+      each<MOST>([&](auto j) {
+        if constexpr (j < PRODUCTS) multiply(first, j);
+        if constexpr (j < FRAGS) read(buf, second, j);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      wait_barrier<(kRing - 2) * LOADS>();
+      // and in the second half by a load of step s + kRing as well
+      each<MOST2>([&](auto j) {
+        if constexpr (j < PRODUCTS) multiply(second, j);
+        if constexpr (j < FRAGS) read(next, first, j);
+        if constexpr (j < LOADS) load(j, buf);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      advance(s + kRing + 1);
+      buf = next;
     }
+  };
+  switch (act) {
+    case 0: sweep(std::integral_constant<int, 0>{}); break;
+    case 1: sweep(std::integral_constant<int, 1>{}); break;
+    case 2: sweep(std::integral_constant<int, MI < 2 ? MI : 2>{}); break;
+    case 3: sweep(std::integral_constant<int, MI < 3 ? MI : 3>{}); break;
+    default: sweep(std::integral_constant<int, MI>{}); break;
   }
 
   // ---- C: lane (r, h) holds row r of a 32-row block, columns 8 i + 4 h .. + 3
   if constexpr (MODE == kBwdW) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the workgroup
     float* c = (float*)(g.part ? a.c2 : a.c) + g.e * wsize;
 #pragma unroll
     for (int m = 0; m < MI; ++m) {
@@ -385,17 +522,19 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
 
 }  // namespace
 
+constexpr int kTallRows = 128;
+
 hipError_t launch_experts_fwd(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_fwd", st);
-  return launch_tiles<kFwd, 128, 128, 2, 2>(a, st);
+  return a.rows / a.E >= kTallRows ? launch_tiles<kFwd, 256, 128, 2, 2>(a, st) : launch_tiles<kFwd, 128, 128, 2, 2>(a, st);
 }
 hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_x", st);
-  return launch_tiles<kBwdX, 128, 128, 2, 2>(a, st);
+  return a.rows / a.E >= kTallRows ? launch_tiles<kBwdX, 256, 128, 2, 2>(a, st) : launch_tiles<kBwdX, 128, 128, 2, 2>(a, st);
 }
 hipError_t launch_experts_bwd_w(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_w", st);
-  return launch_tiles<kBwdW, 128, 128, 2, 2>(a, st);
+  return launch_tiles<kBwdW, 256, 128, 2, 2>(a, st);
 }
 
 }  // namespace spr
