@@ -30,8 +30,6 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 enum ExpertMode { kFwd = 0, kBwdX = 1, kBwdW = 2 };
-constexpr int kStep = 32;   // contraction indices per step
-constexpr int kRing = 3;    // tile buffers
 constexpr int kXcds = 8;
 constexpr int kBand = 4;    // tile rows of a band
 
@@ -39,20 +37,24 @@ __device__ const uint4 zero_line = {0, 0, 0, 0};
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-// Natural operand: ROWS rows of 32 contiguous contraction indices, 64 bytes a
-// row.  Chunk c (16 bytes) of row m lies at chunk c ^ ((m >> 2) & 3): the 16
-// lanes of a read phase then cover 256 bytes once.
-template <int ROWS, int WAVES>
+// Natural operand: ROWS rows of STEP (32 or 64) contiguous contraction indices.
+// Chunk c (16 bytes) of row m lies at chunk c ^ place(m), so that the 16 lanes
+// of a read phase (16 rows, one chunk) cover 256 bytes once.
+template <int ROWS, int STEP, int WAVES>
 struct Natural {
-  static constexpr int N = ROWS / 16, I = (N + WAVES - 1) / WAVES;  // 1 KB loads: of the tile, of a wave
+  static constexpr int CH = STEP / 8, RPL = 64 / CH;  // chunks of a row, rows of a 1 KB load
+  static constexpr int N = ROWS / RPL, I = (N + WAVES - 1) / WAVES;  // loads: of the tile, of a wave
   const char* p[I];
   int col, w;
+  static __device__ __forceinline__ int place(int m) { return STEP == 64 ? swz<64>(m) : (m >> 2) & 3; }
   template <typename RowPtr>
   __device__ __forceinline__ void init(int wave, int lane, RowPtr row_ptr) {
     w = wave;
-    col = 8 * ((lane & 3) ^ ((lane >> 4) & 3));
+    // place() repeats every 16 rows; with 8 rows a load it depends on the load's parity
+    static_assert(STEP == 32 || (WAVES % 2 == 0 && N % 2 == 0), "a wave's loads are all odd or all even");
+    col = 8 * (lane % CH ^ place(RPL * w + lane / CH));
 #pragma unroll
-    for (int i = 0; i < I; ++i) p[i] = (const char*)(row_ptr(16 * ((w + WAVES * i) % N) + (lane >> 2)) + col);
+    for (int i = 0; i < I; ++i) p[i] = (const char*)(row_ptr(RPL * ((w + WAVES * i) % N) + lane / CH) + col);
   }
   __device__ __forceinline__ void advance(long bytes) {
 #pragma unroll
@@ -70,23 +72,24 @@ struct Natural {
   }
   static __device__ __forceinline__ int frag(int lane, int v) {
     const int r = lane & 31, h = lane >> 5;
-    return r * kStep + 8 * ((2 * v + h) ^ ((r >> 2) & 3));
+    return r * STEP + 8 * ((2 * v + h) ^ place(r));
   }
 };
 
-// Transposed operand: 32 contraction rows of COLS columns, in panels of 128.
-template <int COLS, int WAVES>
+// Transposed operand: STEP contraction rows of COLS columns, in panels of 128.
+template <int COLS, int STEP, int WAVES>
 struct Transposed {
-  static constexpr int N = COLS / 16, I = (N + WAVES - 1) / WAVES;
+  static constexpr int PER = STEP / 4;  // loads of a panel, four rows each
+  static constexpr int N = COLS / 128 * PER, I = (N + WAVES - 1) / WAVES;
   const char* p[I];  // column of load i in row 0 of `base`
   int row[I], w;
   __device__ __forceinline__ void init(int wave, int lane, const bf16* base, int ncols) {
     w = wave;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      const int q = (w + WAVES * i) % N;  // panel q / 8, rows 4 (q % 8) ..
-      row[i] = 4 * (q & 7) + (lane >> 4);
-      const int c = 128 * (q >> 3) + 8 * ((lane & 15) ^ swz<128>(row[i]));
+      const int q = (w + WAVES * i) % N;  // panel q / PER, rows 4 (q % PER) ..
+      row[i] = 4 * (q % PER) + (lane >> 4);
+      const int c = 128 * (q / PER) + 8 * ((lane & 15) ^ swz<128>(row[i]));
       p[i] = (const char*)(base + (c < ncols ? c : 0));
     }
   }
@@ -110,7 +113,7 @@ struct Transposed {
   // element offset of 32-column block b's operand, contraction rows 8 h + 4 hi ..
   static __device__ __forceinline__ int frag(int lane, int b, int hi) {
     const int h = lane >> 5, i16 = lane & 15;
-    return (b >> 2) * kStep * 128 +
+    return (b >> 2) * STEP * 128 +
            toff<128>(8 * h + 4 * hi + (i16 >> 2), 32 * (b & 3) + (lane & 16) + 4 * (i16 & 3));
   }
 };
@@ -121,7 +124,7 @@ __device__ __forceinline__ bf16x8 tr_pair(const bf16* lo, const bf16* hi) {
   return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// The tokens of the contraction rows that one wave loads in a step: rows 4 w ..
+// The tokens of the contraction rows that one wave loads in a step of 32: rows 4 w ..
 // and 16 + 4 w .. (rows past the end: token 0, which adds nothing to the address
 // of the line of zeros).  Scalar loads one step ahead of their use: a vector
 // load's wait would also wait for the tiles in flight.
@@ -219,14 +222,16 @@ __device__ __forceinline__ GroupTile find_tile(const ExpertArgs& a, int cols, in
   return g;
 }
 
-template <int MODE, int BM, int BN, int MW, int NW>
-__global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) {
+template <int MODE, int BM, int BN, int MW, int NW, int STEP, int RING>
+__global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) void experts_kernel(ExpertArgs a) {
   constexpr int WAVES = MW * NW, MI = BM / 32 / MW, NI = BN / 32 / NW;
   constexpr bool A_TR = MODE == kBwdW, B_TR = MODE != kBwdX;
-  constexpr int A_ELEMS = BM * kStep, B_ELEMS = BN * kStep;
-  constexpr int LOADS = (BM / 16 + WAVES - 1) / WAVES + (BN / 16 + WAVES - 1) / WAVES;
+  constexpr int A_ELEMS = BM * STEP, B_ELEMS = BN * STEP, SLICES = STEP / 16;
+  constexpr int IA = (BM * STEP / 512 + WAVES - 1) / WAVES, IB = (BN * STEP / 512 + WAVES - 1) / WAVES;
+  constexpr int LOADS = IA + IB;  // a wave's loads of a step
   constexpr int OUT_STRIDE = NI * 32 + 8;  // staged output rows, 16 bytes apart in banks
-  constexpr int STAGE = A_ELEMS + B_ELEMS, SMEM = kRing * STAGE;  // elements
+  constexpr int STAGE = A_ELEMS + B_ELEMS, SMEM = RING * STAGE;  // elements
+  static_assert(!A_TR || STEP == 32, "StepTokens holds 32 rows");
   static_assert(WAVES * 32 * OUT_STRIDE <= SMEM, "the output staging fits the ring");
   __shared__ __attribute__((aligned(1024))) bf16 smem[SMEM];
   const int lane = threadIdx.x & 63, w = wave_id(), wm = w / NW, wn = w % NW;
@@ -259,17 +264,21 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   // this wave's 32-row blocks are wm, wm + MW, ..; act of them have rows
   const int act = clampi((mrows - 32 * wm + 32 * MW - 1) / (32 * MW), 0, MI);
   const int depth = MODE == kFwd ? a.in_width : MODE == kBwdX ? a.out_width : g.len;
-  const int steps1 = (depth + kStep - 1) / kStep;
+  const int steps1 = (depth + STEP - 1) / STEP;
   const int steps = MODE == kBwdX ? steps1 * parts : steps1;
   const size_t wsize = (size_t)a.in_width * a.out_width;
 
   const bool gathers = MODE != kBwdX && a.row_token != nullptr;
 
   // ---- operands
-  Natural<BM, WAVES> an;
-  Transposed<BM, WAVES> at;
-  Natural<BN, WAVES> bn;
-  Transposed<BN, WAVES> bt;
+  typedef Natural<BM, STEP, WAVES> NatA;
+  typedef Natural<BN, STEP, WAVES> NatB;
+  typedef Transposed<BM, STEP, WAVES> TrA;
+  typedef Transposed<BN, STEP, WAVES> TrB;
+  NatA an;
+  TrA at;
+  NatB bn;
+  TrB bt;
   // pointers at the first step of a part
   auto start = [&](int part) {
     if constexpr (!A_TR) {
@@ -298,9 +307,8 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   if constexpr (A_TR)
     if (gathers && steps > 0) tok.fetch(a.row_token, g.lo, 0, g.len, w);
   // The pointers stand at the next step to issue; tok holds its tokens.
-  constexpr int IA = (BM / 16 + WAVES - 1) / WAVES, IB = (BN / 16 + WAVES - 1) / WAVES;
-  const long a_step = A_TR ? 2L * kStep * a.in_width : 2L * kStep;
-  const long b_step = B_TR ? 2L * kStep * a.out_width : 2L * kStep;
+  const long a_step = A_TR ? 2L * STEP * a.in_width : 2L * STEP;
+  const long b_step = B_TR ? 2L * STEP * a.out_width : 2L * STEP;
   auto gathered = [&](int i) -> unsigned long {  // bytes to the row of load i's token
     if (!A_TR || !gathers) return 0;
     return (unsigned long)(unsigned)clampi(tok.of(i, lane), 0, a.x_rows - 1) * (2u * a.in_width);
@@ -325,9 +333,9 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   // steps behind the last one, which the loop issues like all others.
   auto aim = [&](int s) {
     const bool second = MODE == kBwdX && s >= steps1;
-    const int left = s < steps ? depth - (second ? s - steps1 : s) * kStep : 0;
+    const int left = s < steps ? depth - (second ? s - steps1 : s) * STEP : 0;
     if (MODE == kBwdX && s == steps1 && s < steps) start(1);
-    if (left < kStep) {
+    if (left < STEP) {
       if constexpr (A_TR)
         at.stop(left);
       else
@@ -344,7 +352,7 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
     else if (!gathers)
       at.advance(a_step);
     else
-      tok.fetch(a.row_token, g.lo, s * kStep, g.len, w);
+      tok.fetch(a.row_token, g.lo, s * STEP, g.len, w);
     if constexpr (!B_TR)
       bn.advance(b_step);
     else
@@ -352,23 +360,17 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
     aim(s);
   };
 
-  // ---- byte offsets of the operand reads
-  int aoff[2][A_TR ? MI : 1], boff[2][B_TR ? NI : 1];
-#pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    if constexpr (A_TR) {
-#pragma unroll
-      for (int i = 0; i < MI; ++i) aoff[v][i] = 2 * Transposed<BM, WAVES>::frag(lane, i * MW + wm, v);
-    } else {
-      aoff[v][0] = 2 * (Natural<BM, WAVES>::frag(lane, v) + wm * 32 * kStep);
-    }
-    if constexpr (B_TR) {
-#pragma unroll
-      for (int i = 0; i < NI; ++i) boff[v][i] = 2 * Transposed<BN, WAVES>::frag(lane, wn * NI + i, v);
-    } else {
-      boff[v][0] = 2 * (Natural<BN, WAVES>::frag(lane, v) + wn * NI * 32 * kStep);
-    }
-  }
+  // ---- byte offsets of the operand reads: a natural one's per slice, a
+  // transposed one's per 32-column block and row quad
+  int aoff[A_TR ? 2 : SLICES][A_TR ? MI : 1], boff[B_TR ? 2 : SLICES][B_TR ? NI : 1];
+  if constexpr (A_TR)
+    each<2 * MI>([&](auto q) { aoff[q / MI][q % MI] = 2 * TrA::frag(lane, q % MI * MW + wm, q / MI); });
+  else
+    each<SLICES>([&](auto v) { aoff[v][0] = 2 * (NatA::frag(lane, v) + wm * 32 * STEP); });
+  if constexpr (B_TR)
+    each<2 * NI>([&](auto q) { boff[q / NI][q % NI] = 2 * TrB::frag(lane, wn * NI + q % NI, q / NI); });
+  else
+    each<SLICES>([&](auto v) { boff[v][0] = 2 * (NatB::frag(lane, v) + wn * NI * 32 * STEP); });
 
   f32x16 acc[NI][MI];
 #pragma unroll
@@ -376,14 +378,14 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
 #pragma unroll
     for (int m = 0; m < MI; ++m) acc[n][m] = zero16();
 
-  // One half step (16 contraction indices) of operands is read ahead of the
-  // products.  The barrier stands between a step's halves: by then every wave
-  // has read the whole step, so its buffer takes step s + 3 at once, and the
-  // next step, whose loads are waited for there, is read while the second
-  // half's products run.
+  // Operands are read one slice (16 contraction indices) ahead of the products.
+  // The barrier stands before a step's last slice: by then every wave has read
+  // the whole step, so its buffer takes step s + RING at once, and the next
+  // step, whose loads are waited for there, is read while the last slice's
+  // products run.
   if (steps > 0) {
     aim(0);
-    each<kRing>([&](auto s) {
+    each<RING>([&](auto s) {
       each<LOADS>([&](auto j) { load(j, s * STAGE); });
       advance(s + 1);
     });
@@ -393,53 +395,55 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
     bf16x8 fb[2][NI], fa[2][ACT > 0 ? ACT : 1];
     constexpr int FRAGS = ACT > 0 ? ACT + NI : 0, PRODUCTS = ACT * NI;
     constexpr int MOST = PRODUCTS > FRAGS ? PRODUCTS : FRAGS, MOST2 = MOST > LOADS ? MOST : LOADS;
-    // fragment j of half v, in the order of use: b0 a0 b1 .. then the other a
-    auto read = [&](int buf, auto half, auto index) {
-      constexpr int v = decltype(half)::value, j = decltype(index)::value;
+    // fragment j of slice v, in the order of use: b0 a0 b1 .. then the other a
+    auto read = [&](int buf, auto slice, auto index) {
+      constexpr int v = decltype(slice)::value, j = decltype(index)::value;
       const char* ta = (const char*)smem + 2 * buf;
       const char* tb = ta + 2 * A_ELEMS;
       if constexpr (j != 1 && j <= NI) {
         constexpr int n = j == 0 ? 0 : j - 1;
         if constexpr (B_TR)
-          fb[v][n] = tr_pair((const bf16*)(tb + boff[0][n]) + v * 16 * 128, (const bf16*)(tb + boff[1][n]) + v * 16 * 128);
+          fb[v & 1][n] = tr_pair((const bf16*)(tb + boff[0][n]) + v * 16 * 128, (const bf16*)(tb + boff[1][n]) + v * 16 * 128);
         else
-          fb[v][n] = *((const bf16x8*)(tb + boff[v][0]) + n * 4 * kStep);
+          fb[v & 1][n] = *((const bf16x8*)(tb + boff[v][0]) + n * 4 * STEP);
       } else {
         constexpr int m = j == 1 ? 0 : j - NI;
         if constexpr (A_TR)
-          fa[v][m] = tr_pair((const bf16*)(ta + aoff[0][m]) + v * 16 * 128, (const bf16*)(ta + aoff[1][m]) + v * 16 * 128);
+          fa[v & 1][m] = tr_pair((const bf16*)(ta + aoff[0][m]) + v * 16 * 128, (const bf16*)(ta + aoff[1][m]) + v * 16 * 128);
         else
-          fa[v][m] = *((const bf16x8*)(ta + aoff[v][0]) + m * MW * 4 * kStep);
+          fa[v & 1][m] = *((const bf16x8*)(ta + aoff[v][0]) + m * MW * 4 * STEP);
       }
     };
-    auto multiply = [&](auto half, auto index) {
-      constexpr int v = decltype(half)::value, m = decltype(index)::value / NI, n = decltype(index)::value % NI;
-      acc[n][m] = mfma32(fb[v][n], fa[v][m], acc[n][m]);
+    auto multiply = [&](auto slice, auto index) {
+      constexpr int v = decltype(slice)::value, m = decltype(index)::value / NI, n = decltype(index)::value % NI;
+      acc[n][m] = mfma32(fb[v & 1][n], fa[v & 1][m], acc[n][m]);
     };
     const std::integral_constant<int, 0> first{};
-    const std::integral_constant<int, 1> second{};
+    const std::integral_constant<int, SLICES - 1> last{};
     if (steps == 0) return;
-    wait_barrier<(kRing - 1) * LOADS>();
+    wait_barrier<(RING - 1) * LOADS>();
     each<FRAGS>([&](auto j) { read(0, first, j); });
     int buf = 0;
     for (int s = 0; s < steps; ++s) {
       asm volatile("" : "+s"(buf));  // one scalar offset, not a register per address
-      const int next = buf + STAGE < kRing * STAGE ? buf + STAGE : 0;
-      // each product is followed by a read of the other half
-      each<MOST>([&](auto j) {
-        if constexpr (j < PRODUCTS) multiply(first, j);
-        if constexpr (j < FRAGS) read(buf, second, j);
-        __builtin_amdgcn_sched_barrier(0);
+      const int next = buf + STAGE < RING * STAGE ? buf + STAGE : 0;
+      // each product is followed by a read of the next slice
+      each<SLICES - 1>([&](auto v) {
+        each<MOST>([&](auto j) {
+          if constexpr (j < PRODUCTS) multiply(v, j);
+          if constexpr (j < FRAGS) read(buf, std::integral_constant<int, v + 1>{}, j);
+          __builtin_amdgcn_sched_barrier(0);
+        });
       });
-      wait_barrier<(kRing - 2) * LOADS>();
-      // and in the second half by a load of step s + kRing as well
+      wait_barrier<(RING - 2) * LOADS>();
+      // and in the last slice by a load of step s + RING as well
       each<MOST2>([&](auto j) {
-        if constexpr (j < PRODUCTS) multiply(second, j);
+        if constexpr (j < PRODUCTS) multiply(last, j);
         if constexpr (j < FRAGS) read(next, first, j);
         if constexpr (j < LOADS) load(j, buf);
         __builtin_amdgcn_sched_barrier(0);
       });
-      advance(s + kRing + 1);
+      advance(s + RING + 1);
       buf = next;
     }
   };
@@ -501,7 +505,7 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   }
 }
 
-template <int MODE, int BM, int BN, int MW, int NW>
+template <int MODE, int BM, int BN, int MW, int NW, int STEP, int RING>
 hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
   const int ncols = MODE == kBwdX ? a.in_width : a.out_width, parts = a.b2 != nullptr ? 2 : 1;
   const long tiles_n = (ncols + BN - 1) / BN;
@@ -516,7 +520,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
   grid = (grid + kXcds - 1) / kXcds * kXcds;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   if (grid == 0) return hipSuccess;
-  hipLaunchKernelGGL((experts_kernel<MODE, BM, BN, MW, NW>), dim3((unsigned)grid), dim3(64 * MW * NW), 0, st, a);
+  hipLaunchKernelGGL((experts_kernel<MODE, BM, BN, MW, NW, STEP, RING>), dim3((unsigned)grid), dim3(64 * MW * NW), 0, st, a);
   return hipGetLastError();
 }
 
@@ -526,15 +530,15 @@ constexpr int kTallRows = 128;
 
 hipError_t launch_experts_fwd(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_fwd", st);
-  return a.rows / a.E >= kTallRows ? launch_tiles<kFwd, 256, 128, 2, 2>(a, st) : launch_tiles<kFwd, 128, 128, 2, 2>(a, st);
+  return a.rows / a.E >= kTallRows ? launch_tiles<kFwd, 256, 256, 2, 4, 64, 2>(a, st) : launch_tiles<kFwd, 128, 128, 2, 2, 64, 2>(a, st);
 }
 hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_x", st);
-  return a.rows / a.E >= kTallRows ? launch_tiles<kBwdX, 256, 128, 2, 2>(a, st) : launch_tiles<kBwdX, 128, 128, 2, 2>(a, st);
+  return a.rows / a.E >= kTallRows ? launch_tiles<kBwdX, 256, 256, 2, 4, 64, 2>(a, st) : launch_tiles<kBwdX, 128, 128, 2, 2, 64, 2>(a, st);
 }
 hipError_t launch_experts_bwd_w(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_w", st);
-  return launch_tiles<kBwdW, 256, 128, 2, 2>(a, st);
+  return launch_tiles<kBwdW, 256, 128, 2, 2, 32, 3>(a, st);
 }
 
 }  // namespace spr
