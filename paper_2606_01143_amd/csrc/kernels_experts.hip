@@ -124,13 +124,15 @@ __device__ __forceinline__ bf16x8 tr_pair(const bf16* lo, const bf16* hi) {
   return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// The tokens of the contraction rows that one wave loads in a step of 32: rows 4 w ..
-// and, of four waves, 16 + 4 w .. (rows past the end: token 0, which adds nothing to the address
-// of the line of zeros).  Scalar loads one step ahead of their use: a vector
-// load's wait would also wait for the tiles in flight.
-template <int WAVES>
+// The tokens of the contraction rows that one wave loads in a step: rows 4 w ..
+// and, where a panel has more loads than there are waves, 4 (WAVES + w) .. (rows
+// past the end: token 0, which adds nothing to the address of the line of
+// zeros).  Scalar loads one step ahead of their use: a vector load's wait would
+// also wait for the tiles in flight.
+template <int WAVES, int STEP>
 struct StepTokens {
-  static_assert(WAVES == 4 || WAVES == 8, "a wave's loads cover one or two groups of four rows");
+  static constexpr bool TWO = STEP / 4 == 2 * WAVES;
+  static_assert(TWO || STEP / 4 == WAVES, "a wave's loads cover one or two groups of four rows");
   i32x4 lo4, hi4;  // vectors, not arrays: those would be moved to LDS
   __device__ __forceinline__ void fetch(const int32_t* row_token, int lo, int k0, int len, int w) {
     typedef const __attribute__((address_space(4))) int32_t scalar_int;
@@ -138,21 +140,21 @@ struct StepTokens {
     typedef const __attribute__((address_space(4))) quad scalar_quad;
     const uintptr_t src = (uintptr_t)(row_token + lo);
     const int k = k0 + 4 * w, last = len - 1;
-    if (k0 + 32 <= len) {
+    if (k0 + STEP <= len) {
       lo4 = *(scalar_quad*)(src + 4L * k);
-      if constexpr (WAVES == 4) hi4 = *(scalar_quad*)(src + 4L * (k + 16));
+      if constexpr (TWO) hi4 = *(scalar_quad*)(src + 4L * (k + 4 * WAVES));
     } else {
       auto at = [&](int q) {
         const int t = ((scalar_int*)src)[min(k + q, last)];
         return k + q < len ? t : 0;
       };
       lo4 = i32x4{at(0), at(1), at(2), at(3)};
-      if constexpr (WAVES == 4) hi4 = i32x4{at(16), at(17), at(18), at(19)};
+      if constexpr (TWO) hi4 = i32x4{at(4 * WAVES), at(4 * WAVES + 1), at(4 * WAVES + 2), at(4 * WAVES + 3)};
     }
   }
   // of load i, this lane's row
   __device__ __forceinline__ int of(int i, int lane) const {
-    const i32x4 v = WAVES == 4 && (i & 1) ? hi4 : lo4;
+    const i32x4 v = TWO && (i & 1) ? hi4 : lo4;
     const int a = lane & 16 ? v[1] : v[0], b = lane & 16 ? v[3] : v[2];
     return lane & 32 ? b : a;
   }
@@ -232,6 +234,9 @@ __device__ __forceinline__ GroupTile find_tile(const ExpertArgs& a, int cols, in
   return g;
 }
 
+// an XCD's tiles of an expert in bwd_w
+__host__ __device__ __forceinline__ int bwd_w_share(int tiles) { return (tiles + kXcds - 1) / kXcds; }
+
 // TOKENS: the contraction rows of bwd_w are gathered
 template <int MODE, int BM, int BN, int MW, int NW, int STEP, int RING, bool TOKENS>
 __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) void experts_kernel(ExpertArgs a) {
@@ -240,9 +245,10 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
   constexpr int A_ELEMS = BM * STEP, B_ELEMS = BN * STEP, SLICES = STEP / 16;
   constexpr int IA = (BM * STEP / 512 + WAVES - 1) / WAVES, IB = (BN * STEP / 512 + WAVES - 1) / WAVES;
   constexpr int LOADS = IA + IB;  // a wave's loads of a step
+  // of which so many are issued in the last slice, the others in the next step's first
+  constexpr int EARLY = STEP == 64 ? LOADS / 2 : LOADS;
   constexpr int OUT_STRIDE = NI * 32 + 8;  // staged output rows, 16 bytes apart in banks
   constexpr int SMEM = RING * (A_ELEMS + B_ELEMS);  // elements: the A tiles, then the B tiles
-  static_assert(!A_TR || STEP == 32, "StepTokens holds 32 rows");
   static_assert(WAVES * 32 * OUT_STRIDE <= SMEM, "the output staging fits the ring");
   __shared__ __attribute__((aligned(1024))) bf16 smem[SMEM];
   const int lane = threadIdx.x & 63, w = wave_id(), wm = w / NW, wn = w % NW;
@@ -253,14 +259,19 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
 
   GroupTile g;
   if constexpr (MODE == kBwdW) {
-    const int tiles_m = (a.in_width + BM - 1) / BM;
-    const long total = (long)a.E * parts * tiles_n * tiles_m, chunk = (total + kXcds - 1) / kXcds;
-    const long at = blockIdx.x / kXcds, t = (blockIdx.x % kXcds) * chunk + at;
-    if (at >= chunk || t >= total) return;
-    g.m0 = (int)(t % tiles_m) * BM;
-    g.n0 = (int)(t / tiles_m % tiles_n) * BN;
-    g.part = (int)(t / tiles_m / tiles_n % parts);
-    g.e = (int)(t / tiles_m / tiles_n / parts);
+    // Every XCD takes an eighth of every expert's tiles, because an expert's
+    // tiles take as long as it has rows; the eighths turn with the expert, so
+    // that short last ones meet every XCD.  (Whole experts per XCD: 18% of the
+    // time idle at 128 experts of unequal sizes, 49% at eight.)
+    const int tiles_m = (a.in_width + BM - 1) / BM, cols = tiles_n * parts, per = bwd_w_share(tiles_m * cols);
+    const int xcd = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
+    g.e = at / per;
+    const int left = (xcd + g.e) % kXcds * per + at % per;
+    if (left >= tiles_m * cols) return;
+    const int band = left / (kBand * cols), in = left % (kBand * cols), high = min(kBand, tiles_m - band * kBand);
+    g.m0 = (band * kBand + in % high) * BM;
+    g.n0 = in / high % tiles_n * BN;
+    g.part = in / high / tiles_n;
     g.lo = clampi(a.offsets[g.e], 0, a.rows);
     g.len = clampi(a.offsets[g.e + 1], g.lo, a.rows) - g.lo;
     if (g.len == 0 && !a.overwrite) return;
@@ -314,7 +325,7 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
     }
   };
   start(0);
-  StepTokens<A_TR ? WAVES : 4> tok;
+  StepTokens<TOKENS ? WAVES : 8, TOKENS ? STEP : 32> tok;
   if constexpr (TOKENS)
     if (steps > 0) tok.fetch(a.row_token, g.lo, 0, g.len, w);
   // The pointers stand at the next step to issue; tok holds its tokens.
@@ -402,8 +413,10 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
   if (steps > 0) {
     aim(0);
     each<RING>([&](auto s) {
-      each<LOADS>([&](auto j) { load(j, s); });
-      advance(s + 1);
+      each<LOADS>([&](auto j) {
+        if constexpr (s < RING - 1 || j < EARLY) load(j, s);
+      });
+      if constexpr (s < RING - 1) advance(s + 1);
     });
   }
   auto sweep = [&](auto active) {
@@ -436,7 +449,7 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
     const std::integral_constant<int, 0> first{};
     const std::integral_constant<int, SLICES - 1> last{};
     if (steps == 0) return;
-    wait_barrier<(RING - 1) * LOADS>();
+    wait_barrier<(RING - 2) * LOADS + EARLY>();
     each<FRAGS>([&](auto j) { read(first, first, j); });
     // one round of the ring: a buffer's offset is part of each read instruction
     for (int s = 0; s < steps;) {
@@ -444,23 +457,26 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
         if (s >= steps) return;
         constexpr int b = decltype(buffer)::value;
         const std::integral_constant<int, b + 1 < RING ? b + 1 : 0> next{};
-        // each product is followed by a read of the next slice
+        const std::integral_constant<int, (b + RING - 1) % RING> previous{};
+        // each product is followed by a read of the next slice, and in the first
+        // one by a load of the second half of step s + RING - 1
         each<SLICES - 1>([&](auto v) {
-          each<MOST>([&](auto j) {
+          each<MOST2>([&](auto j) {
             if constexpr (j < PRODUCTS) multiply(v, j);
             if constexpr (j < FRAGS) read(buffer, std::integral_constant<int, v + 1>{}, j);
+            if constexpr (v == 0 && EARLY + j < LOADS) load(std::integral_constant<int, EARLY + j>{}, previous);
             __builtin_amdgcn_sched_barrier(0);
           });
+          if constexpr (v == 0) advance(s + RING);
         });
         wait_barrier<(RING - 2) * LOADS>();
-        // and in the last slice by a load of step s + RING as well
+        // in the last one by a load of the first half of step s + RING
         each<MOST2>([&](auto j) {
           if constexpr (j < PRODUCTS) multiply(last, j);
           if constexpr (j < FRAGS) read(next, first, j);
-          if constexpr (j < LOADS) load(j, buffer);
+          if constexpr (j < EARLY) load(j, buffer);
           __builtin_amdgcn_sched_barrier(0);
         });
-        advance(s + RING + 1);
         ++s;
       });
     }
@@ -555,7 +571,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
   const long tiles_n = (ncols + BN - 1) / BN;
   long grid;
   if (MODE == kBwdW) {
-    grid = (long)a.E * parts * tiles_n * ((a.in_width + BM - 1) / BM);
+    grid = (long)kXcds * a.E * bwd_w_share((int)(parts * tiles_n * ((a.in_width + BM - 1) / BM)));
   } else {
     // at most a partial tile of rows for every expert that has any
     const long some = a.E < a.rows ? a.E : a.rows;
@@ -582,7 +598,7 @@ hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st) {
 }
 hipError_t launch_experts_bwd_w(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_w", st);
-  return a.row_token != nullptr ? launch_tiles<kBwdW, 256, 256, 2, 4, 32, 3, true>(a, st)
+  return a.row_token != nullptr ? launch_tiles<kBwdW, 256, 256, 2, 4, 64, 2, true>(a, st)
                                 : launch_tiles<kBwdW, 256, 256, 2, 4, 32, 3>(a, st);
 }
 
