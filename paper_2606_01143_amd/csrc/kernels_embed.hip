@@ -79,48 +79,149 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int* __r
   });
 }
 
-// the thread of a run's first sorted token adds up one chunk of the run
+// Sums of runs (the sorted tokens of one id).  A wave takes kSpan consecutive
+// sorted tokens and 512 columns (eight a lane), so that a frequent id's run is
+// shared by many waves.  A run that lies inside the span is added to its table
+// row at once; the part of one that began before it goes to head[span], the part
+// of one that begins here and goes on to tail[span], and embed_join adds those up
+// in order.  Per element that is the order of the tokens within a span, then of
+// the spans.  HBM bound: a row of dy is read once, a row of the table read and
+// written once, a part (at most two a span) written and read once.
+constexpr int kSpan = 32, kAhead = 4;
+
 template <typename T>
-__global__ __launch_bounds__(kEmbedThreads) void embed_bwd_kernel(const int* __restrict__ keys,
-                                                                  const int* __restrict__ order,
-                                                                  const T* __restrict__ dy,
-                                                                  float* __restrict__ dtable, long tokens, int vocab,
-                                                                  int chunks, float scale) {
-  const long i = (long)blockIdx.x * kEmbedThreads + threadIdx.x;
-  if (i >= tokens * chunks) return;
-  const long p = i / chunks, c = i % chunks;
-  const int key = keys[p];
-  if (key >= vocab || (p > 0 && keys[p - 1] == key)) return;
+__global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(const int* __restrict__ keys,
+                                                                   const int* __restrict__ order,
+                                                                   const T* __restrict__ dy, float* dtable,
+                                                                   float* __restrict__ head, float* __restrict__ tail,
+                                                                   int tokens, int vocab, int chunks, int slabs,
+                                                                   float scale) {
+  const long wave = (long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long span = wave / slabs;
+  const int lane = threadIdx.x & 63, chunk = (int)(wave % slabs) * 64 + lane;
+  const long p0 = span * kSpan;
+  if (p0 >= tokens) return;
+  const int n = (int)min((long)kSpan, tokens - p0);
+  // lane q holds the span's q-th key and token, lane kSpan the key behind it, and
+  // the one after that the key before it
+  int key = vocab, token = 0;
+  if (lane < n) {
+    key = keys[p0 + lane];
+    token = order[p0 + lane];
+  } else if (lane == kSpan && p0 + kSpan < tokens) {
+    key = keys[p0 + kSpan];
+  } else if (lane == kSpan + 1 && p0 > 0) {
+    key = keys[p0 - 1];
+  }
+  auto key_at = [&](int q) { return __builtin_amdgcn_readlane(key, q); };
+  const int behind = n == kSpan ? key_at(kSpan) : vocab, before = p0 > 0 ? key_at(kSpan + 1) : vocab;
+  const bool in = chunk < chunks;
   float sum[8] = {};
-  for (long q = p; q < tokens && keys[q] == key; ++q) {
+  float v[kAhead][8];
+  auto fetch = [&](int q, float (&to)[8]) {
+    const int t = __builtin_amdgcn_readlane(token, q);
+    if (in) Vec8<T>::load(dy + ((long)t * chunks + chunk) * 8, to);
+  };
+#pragma unroll
+  for (int q = 0; q < kAhead; ++q)
+    if (q < n && key_at(q) < vocab) fetch(q, v[q]);
+  bool first = true;  // of the run that the sum holds: it begins the span
+  for (int q0 = 0; q0 < n; q0 += kAhead) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int q = q0 + u;
+      if (q >= n) break;
+      const int k = key_at(q);
+      if (k >= vocab) return;  // dropped tokens are the last ones
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
+      if (q + kAhead < n && key_at(q + kAhead) < vocab) fetch(q + kAhead, v[u]);
+      const int next = q + 1 < n ? key_at(q + 1) : behind;
+      if (next == k && q + 1 < n) continue;
+      if (in) {
+        if (first && before == k) {
+          Vec8<float>::store(head + (span * chunks + chunk) * 8, sum);
+        } else if (next == k) {
+          Vec8<float>::store(tail + (span * chunks + chunk) * 8, sum);
+        } else {
+          float* dst = dtable + ((long)k * chunks + chunk) * 8;
+          float old[8];
+          Vec8<float>::load(dst, old);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) old[j] = fmaf(scale, sum[j], old[j]);
+          Vec8<float>::store(dst, old);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+      first = false;
+    }
+  }
+}
+
+// The runs that cross spans: the wave of the span where one begins adds its
+// tail and the heads of the spans up to its end, eight at a time.
+__global__ __launch_bounds__(kEmbedThreads) void embed_join_kernel(const int* __restrict__ keys, float* dtable,
+                                                                   const float* __restrict__ head,
+                                                                   const float* __restrict__ tail, int tokens,
+                                                                   int vocab, int chunks, int slabs, float scale) {
+  const long wave = (long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long span = wave / slabs, p0 = span * kSpan;
+  const int lane = threadIdx.x & 63, chunk = (int)(wave % slabs) * 64 + lane;
+  if (p0 + kSpan >= tokens) return;
+  const int k = keys[p0 + kSpan - 1];
+  // a run begins here and goes on
+  if (k >= vocab || keys[p0 + kSpan] != k || (p0 > 0 && keys[p0] == k && keys[p0 - 1] == k)) return;
+  // its last span: the first one behind this whose last key is another, found
+  // 64 spans at a time
+  const long spans = (tokens + kSpan - 1) / kSpan;
+  long end = span;
+  for (long s = span + 1;; s += 64) {
+    const long mine = s + lane;
+    const bool on = mine + 1 < spans && keys[mine * kSpan + kSpan - 1] == k && keys[mine * kSpan + kSpan] == k;
+    const unsigned long long off = __ballot(!on);
+    if (off != 0) {
+      end = s + __builtin_ctzll(off);
+      break;
+    }
+  }
+  if (chunk >= chunks) return;
+  float sum[8];
+  Vec8<float>::load(tail + (span * chunks + chunk) * 8, sum);
+#pragma unroll 8
+  for (long s = span + 1; s <= end; ++s) {
     float v[8];
-    Vec8<T>::load(dy + ((long)order[q] * chunks + c) * 8, v);
+    Vec8<float>::load(head + (s * chunks + chunk) * 8, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] += v[j];
   }
-  float* dst = dtable + ((long)key * chunks + c) * 8;
-  float v[8];
-  Vec8<float>::load(dst, v);
+  float* dst = dtable + ((long)k * chunks + chunk) * 8;
+  float old[8];
+  Vec8<float>::load(dst, old);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = fmaf(scale, sum[j], v[j]);
-  Vec8<float>::store(dst, v);
+  for (int j = 0; j < 8; ++j) old[j] = fmaf(scale, sum[j], old[j]);
+  Vec8<float>::store(dst, old);
 }
 
 namespace {
-// workspace: two buffers of keys and tokens, then the histograms
+// workspace: two buffers of keys and tokens, the histograms, then the parts of
+// runs that cross spans (none where one span holds all tokens)
 struct EmbedWs {
-  size_t item, hist, total;
+  size_t item, hist, head, tail, total;
 };
-EmbedWs embed_ws(long n) {
+EmbedWs embed_ws(long n, long width) {
   EmbedWs w;
   w.item = ((size_t)n * 4 + 255) / 256 * 256;
   w.hist = 4 * w.item;
-  w.total = w.hist + sort_hist_bytes(n, 1 << kSortRadixBits);
+  w.head = w.hist + (sort_hist_bytes(n, 1 << kSortRadixBits) + 255) / 256 * 256;
+  const size_t part = n > kSpan ? (size_t)((n + kSpan - 1) / kSpan) * width * 4 : 0;
+  w.tail = w.head + part;
+  w.total = w.tail + part;
   return w;
 }
 }  // namespace
 
-size_t embed_bwd_ws(long tokens, int vocab, int width) { return tokens == 0 ? 0 : embed_ws(tokens).total; }
+size_t embed_bwd_ws(long tokens, int vocab, int width) { return tokens == 0 ? 0 : embed_ws(tokens, width).total; }
 
 hipError_t launch_embed_fwd(int dtype, int tokens, int vocab, int width, float scale, const int* ids,
                             const void* table, void* y, hipStream_t st) {
@@ -141,7 +242,7 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
                             float* dtable, void* ws, hipStream_t st) {
   const long n = tokens;
   if (n == 0) return hipSuccess;
-  const EmbedWs w = embed_ws(n);
+  const EmbedWs w = embed_ws(n, width);
   char* base = (char*)ws;
   int* keys[2] = {(int*)base, (int*)(base + w.item)};
   int* order[2] = {(int*)(base + 2 * w.item), (int*)(base + 3 * w.item)};
@@ -164,15 +265,25 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
       out ^= 1;
     }
   }
-  ProfileScope ps("embed_bwd", st);
-  const long m = n * (width / 8);
-  const dim3 grid((unsigned)((m + kEmbedThreads - 1) / kEmbedThreads));
-  if (dtype == 1)
-    hipLaunchKernelGGL(embed_bwd_kernel<bf16>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const bf16*)dy, dtable,
-                       n, vocab, width / 8, scale);
-  else
-    hipLaunchKernelGGL(embed_bwd_kernel<float>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const float*)dy,
-                       dtable, n, vocab, width / 8, scale);
+  const int chunks = width / 8, slabs = (chunks + 63) / 64;
+  float* head = (float*)(base + w.head);
+  float* tail = (float*)(base + w.tail);
+  const long waves = (n + kSpan - 1) / kSpan * slabs;
+  const dim3 grid((unsigned)((waves + kEmbedThreads / 64 - 1) / (kEmbedThreads / 64)));
+  {
+    ProfileScope ps("embed_runs", st);
+    if (dtype == 1)
+      hipLaunchKernelGGL(embed_runs_kernel<bf16>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const bf16*)dy,
+                         dtable, head, tail, tokens, vocab, chunks, slabs, scale);
+    else
+      hipLaunchKernelGGL(embed_runs_kernel<float>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const float*)dy,
+                         dtable, head, tail, tokens, vocab, chunks, slabs, scale);
+  }
+  if (n > kSpan) {
+    ProfileScope ps("embed_join", st);
+    hipLaunchKernelGGL(embed_join_kernel, grid, dim3(kEmbedThreads), 0, st, k_in, dtable, head, tail, tokens, vocab,
+                       chunks, slabs, scale);
+  }
   return hipGetLastError();
 }
 
