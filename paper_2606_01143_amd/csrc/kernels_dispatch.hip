@@ -22,18 +22,14 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
 
 // One pass of the stable sort with a bin per expert; dropped choices are the
 // last bin, whose start is offsets[E].
-__global__ __launch_bounds__(kSortThreads) void experts_plan_kernel(const int* __restrict__ experts, long n, long per,
-                                                                    int E, int k, int bits, int nb,
-                                                                    const int* __restrict__ hist,
-                                                                    int* __restrict__ offsets,
+__global__ __launch_bounds__(kSortThreads) void experts_plan_kernel(SortPass p, int k, int* __restrict__ offsets,
                                                                     int* __restrict__ row_token,
                                                                     int* __restrict__ pos) {
   __shared__ SortLds s;
-  sort_bases(s, hist, E + 1, nb, blockIdx.x, offsets);
-  const long lo = blockIdx.x * per;
-  sort_walk(s, experts, lo, min(n, lo + per), E, 0, -1, bits, [&](long i, int key, int place) {
-    row_token[place] = key < E ? (int)(i / k) : -1;
-    pos[i] = key < E ? place : -1;
+  sort_bases(s, p, offsets);
+  sort_walk(s, p, [&](long i, int key, int place) {
+    row_token[place] = key < p.limit ? (int)((unsigned)i / (unsigned)k) : -1;
+    pos[i] = key < p.limit ? place : -1;
   });
 }
 
@@ -107,13 +103,14 @@ size_t experts_plan_ws(int E, long slots) { return sort_hist_bytes(slots, E + 1)
 
 hipError_t launch_experts_plan(int E, int k, long slots, const int* experts, int* offsets, int* row_token, int* pos,
                                void* ws, hipStream_t st) {
+  const int nb = sort_ranges(slots);
+  const SortPass p = {experts, slots, sort_range_items(slots, nb), E, 0, sort_bits(E), E + 1, nb, (int*)ws};
+  if (nb > 1) {
+    ProfileScope ps("sort_count", st);
+    hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, p);
+  }
   ProfileScope ps("experts_plan", st);
-  const int nb = sort_ranges(slots), bins = E + 1;
-  const long per = sort_range_items(slots, nb);
-  hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, experts, slots, per, E, 0, bins, -1,
-                     (int*)ws);
-  hipLaunchKernelGGL(experts_plan_kernel, dim3(nb), dim3(kSortThreads), 0, st, experts, slots, per, E, k,
-                     sort_bits(E), nb, (const int*)ws, offsets, row_token, pos);
+  hipLaunchKernelGGL(experts_plan_kernel, dim3(nb), dim3(kSortThreads), 0, st, p, k, offsets, row_token, pos);
   return hipGetLastError();
 }
 

@@ -64,16 +64,12 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(const int* __r
 }
 
 // one pass of the sort: keys and the tokens they belong to
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int* __restrict__ keys,
-                                                                  const int* __restrict__ tokens, long n, long per,
-                                                                  int limit, int shift, int bins, int mask, int bits,
-                                                                  int nb, const int* __restrict__ hist,
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortPass p, const int* __restrict__ tokens,
                                                                   int* __restrict__ keys_out,
                                                                   int* __restrict__ tokens_out) {
   __shared__ SortLds s;
-  sort_bases(s, hist, bins, nb, blockIdx.x, nullptr);
-  const long lo = blockIdx.x * per;
-  sort_walk(s, keys, lo, min(n, lo + per), limit, shift, mask, bits, [&](long i, int key, int place) {
+  sort_bases(s, p, nullptr);
+  sort_walk(s, p, [&](long i, int key, int place) {
     keys_out[place] = key;
     tokens_out[place] = tokens ? tokens[i] : (int)i;
   });
@@ -252,18 +248,18 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
   const int* k_in = ids;
   const int* t_in = nullptr;
   int out = 0;
-  {
-    ProfileScope ps("embed_sort", st);
-    for (int shift = 0, left = sort_bits(vocab); left > 0; left -= kSortRadixBits, shift += kSortRadixBits) {
-      const int bits = left < kSortRadixBits ? left : kSortRadixBits, bins = 1 << bits, mask = bins - 1;
-      hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, k_in, n, per, vocab, shift, bins,
-                         mask, hist);
-      hipLaunchKernelGGL(embed_sort_kernel, dim3(nb), dim3(kSortThreads), 0, st, k_in, t_in, n, per, vocab, shift,
-                         bins, mask, bits, nb, hist, keys[out], order[out]);
-      k_in = keys[out];
-      t_in = order[out];
-      out ^= 1;
+  for (int shift = 0, left = sort_bits(vocab); left > 0; left -= kSortRadixBits, shift += kSortRadixBits) {
+    const int bits = left < kSortRadixBits ? left : kSortRadixBits;
+    const SortPass p = {k_in, n, per, vocab, shift, bits, 1 << bits, nb, hist};
+    if (nb > 1) {
+      ProfileScope ps("sort_count", st);
+      hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, p);
     }
+    ProfileScope ps("embed_sort", st);
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(nb), dim3(kSortThreads), 0, st, p, t_in, keys[out], order[out]);
+    k_in = keys[out];
+    t_in = order[out];
+    out ^= 1;
   }
   const int chunks = width / 8, slabs = (chunks + 63) / 64;
   float* head = (float*)(base + w.head);
