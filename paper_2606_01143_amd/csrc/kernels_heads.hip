@@ -9,6 +9,8 @@
 // keeps nothing.  Sums, norms and angles are fp32 (the angle's reduction fp64).
 #include <math.h>
 
+#include <algorithm>
+
 #include "launch.hpp"
 
 namespace spr {
@@ -38,6 +40,7 @@ __device__ __forceinline__ double head_pos(const HeadArgs& a, long t) {
 }
 }  // namespace
 
+// ------------------------------------------------ any head dim and alignment
 // One wave per row; lane l has the pairs l and l + 64.
 template <typename T>
 __global__ __launch_bounds__(kHeadThreads) void head_norm_rope_fwd_kernel(HeadArgs a) {
@@ -145,30 +148,338 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm_rope_bwd_kernel(HeadAr
   }
 }
 
-// dgain (+)= the sum of part over its blocks, in block order within sixteen
-// interleaved slices; 64 columns of the 2 d per workgroup
+// ------------------------------------------------ rows of 16-byte chunks
+// Head dims that are a multiple of 16, with 16-byte rows: a wave takes a token
+// at a time (or a share of its heads, where there are few tokens).  A head's row
+// is held by G lanes (a power of two, d / 16 of them used), eight values of
+// either half each, so that a pair's two values meet in one lane; the row's sums
+// take log2 G shuffles.  The token's angles are formed once, one pair a lane,
+// and shared by its heads through LDS; the frequencies once a wave.  The next
+// rows are loaded before the present ones are worked on.
+// HBM bound: FORWARD
+namespace {
+template <typename T>
+struct Chunk;
+template <>
+struct Chunk<bf16> {
+  bf16x8 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *(const bf16x8*)p; }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (bf16)0.f;
+  }
+  __device__ __forceinline__ float at(int j) const { return (float)v[j]; }
+  static __device__ __forceinline__ void store(bf16* p, const float (&x)[8]) {
+    bf16x8 o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (bf16)x[j];
+    *(bf16x8*)p = o;
+  }
+};
+template <>
+struct Chunk<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = ((const f32x4*)p)[0];
+    b = ((const f32x4*)p)[1];
+  }
+  __device__ __forceinline__ void zero() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ float at(int j) const { return j < 4 ? a[j] : b[j - 4]; }
+  static __device__ __forceinline__ void store(float* p, const float (&x)[8]) {
+    ((f32x4*)p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+    ((f32x4*)p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+  }
+};
+
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// A lane's place in its wave's rows and what it needs of every token.
+template <typename T, int G>
+struct RowLane {
+  static constexpr int kHeads = 64 / G;  // heads a wave holds at once
+  int lane, c, col, half;                // chunk of either half, its first column
+  bool used;
+  double turns[kMaxPairs];               // of the pairs lane and lane + 64, per position
+  float cs[8], sn[8];
+  __device__ __forceinline__ RowLane(const HeadArgs& a) {
+    lane = threadIdx.x & 63;
+    c = lane % G;
+    col = 8 * c;
+    half = a.d / 2;
+    used = col < half;
+#pragma unroll
+    for (int q = 0; q < kMaxPairs; ++q) turns[q] = exp2((double)(lane + 64 * q) * a.log2_step) * (0.5 / M_PI);
+  }
+  // the angles of token t, through the wave's own LDS
+  __device__ __forceinline__ void angles(const HeadArgs& a, long t, float2* shared) {
+    const double pos = head_pos(a, t);
+    __builtin_amdgcn_wave_barrier();  // the last token's have been read
+#pragma unroll
+    for (int q = 0; q < kMaxPairs; ++q) {
+      if (64 * q < half) {
+        const double n = pos * turns[q];
+        float s, k;
+        sincospif((float)(2.0 * (n - rint(n))), &s, &k);
+        if (lane + 64 * q < half) shared[lane + 64 * q] = make_float2(k, s);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 v = shared[used ? col + j : 0];
+      cs[j] = v.x;
+      sn[j] = v.y;
+    }
+  }
+  // gain values of the chunk: [0, 8) of the lower half, [8, 16) of the upper
+  __device__ __forceinline__ void gains(const T* g, float (&out)[16]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      out[j] = used ? to_f32(g[col + j]) : 0.f;
+      out[8 + j] = used ? to_f32(g[col + half + j]) : 0.f;
+    }
+  }
+};
+
+// rounds of `heads` heads, kHeads at a time, that share `part` of `parts` takes
+// of q's and k's rounds together
+struct Rounds {
+  int q0, q1, k0, k1;
+};
+__device__ __forceinline__ Rounds rounds_of(const HeadArgs& a, int heads, int part, int parts) {
+  const int nq = (a.hq + heads - 1) / heads, n = nq + (a.hkv + heads - 1) / heads, per = (n + parts - 1) / parts;
+  const int lo = min(part * per, n), hi = min(lo + per, n);
+  return {min(lo, nq), min(hi, nq), max(lo, nq) - nq, max(hi, nq) - nq};
+}
+}  // namespace
+
+template <typename T, int G>
+__global__ __launch_bounds__(kHeadThreads) void head_rows_fwd_kernel(HeadArgs a, int parts) {
+  __shared__ float2 shared[kHeadWaves][64 * kMaxPairs];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowLane<T, G> l(a);
+  float gq[16], gk[16];
+  l.gains((const T*)a.gain_q, gq);
+  l.gains((const T*)a.gain_k, gk);
+  const long units = (long)a.tokens * parts, stride = (long)gridDim.x * kHeadWaves;
+  for (long u = (long)blockIdx.x * kHeadWaves + w; u < units; u += stride) {
+    const long t = u / parts;
+    const Rounds n = rounds_of(a, RowLane<T, G>::kHeads, (int)(u % parts), parts);
+    auto sweep = [&](int r0, int r1, const T* x, T* y, int heads, const float (&g)[16], auto&& first) {
+      Chunk<T> lo, hi, lo2, hi2;
+      auto fetch = [&](int r, Chunk<T>& p, Chunk<T>& q) {
+        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
+        p.zero();
+        q.zero();
+        if (l.used && h < heads) {
+          p.load(x + (long)h * a.d + l.col);
+          q.load(x + (long)h * a.d + l.col + l.half);
+        }
+      };
+      if (r0 < r1) fetch(r0, lo, hi);
+      first();
+      for (int r = r0; r < r1; ++r) {
+        if (r + 1 < r1) fetch(r + 1, lo2, hi2);
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ss = fmaf(lo.at(j), lo.at(j), fmaf(hi.at(j), hi.at(j), ss));
+        const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
+        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
+        if (l.used && h < heads) {
+          float p[8], q[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float u0 = lo.at(j) * rs * g[j], u1 = hi.at(j) * rs * g[8 + j];
+            p[j] = u0 * l.cs[j] - u1 * l.sn[j];
+            q[j] = u1 * l.cs[j] + u0 * l.sn[j];
+          }
+          Chunk<T>::store(y + (long)h * a.d + l.col, p);
+          Chunk<T>::store(y + (long)h * a.d + l.col + l.half, q);
+        }
+        lo = lo2;
+        hi = hi2;
+      }
+    };
+    // the first rows are on their way while the angles are formed
+    bool formed = false;
+    auto angles = [&] {
+      if (!formed) l.angles(a, t, shared[w]);
+      formed = true;
+    };
+    sweep(n.q0, n.q1, (const T*)a.q + t * a.q_stride, (T*)a.yq + t * a.hq * a.d, a.hq, gq, angles);
+    sweep(n.k0, n.k1, (const T*)a.k + t * a.k_stride, (T*)a.yk + t * a.hkv * a.d, a.hkv, gk, angles);
+  }
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(kHeadThreads) void head_rows_bwd_kernel(HeadArgs a, int parts) {
+  __shared__ float2 shared[kHeadWaves][64 * kMaxPairs];
+  __shared__ float red[kHeadWaves][2][2 * 64 * kMaxPairs];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowLane<T, G> l(a);
+  float gq[16], gk[16], dgq[16] = {}, dgk[16] = {};
+  l.gains((const T*)a.gain_q, gq);
+  l.gains((const T*)a.gain_k, gk);
+  const long units = (long)a.tokens * parts, stride = (long)gridDim.x * kHeadWaves;
+  for (long u = (long)blockIdx.x * kHeadWaves + w; u < units; u += stride) {
+    const long t = u / parts;
+    const Rounds n = rounds_of(a, RowLane<T, G>::kHeads, (int)(u % parts), parts);
+    auto sweep = [&](int r0, int r1, const T* x, const T* dy, T* dx, int heads, const float (&g)[16], float (&dg)[16],
+                     auto&& first) {
+      Chunk<T> xl, xh, yl, yh, xl2, xh2, yl2, yh2;
+      auto fetch = [&](int r, Chunk<T>& p, Chunk<T>& q, Chunk<T>& e, Chunk<T>& f) {
+        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
+        p.zero();
+        q.zero();
+        e.zero();
+        f.zero();
+        if (l.used && h < heads) {
+          const long at = (long)h * a.d + l.col;
+          p.load(x + at);
+          q.load(x + at + l.half);
+          e.load(dy + at);
+          f.load(dy + at + l.half);
+        }
+      };
+      if (r0 < r1) fetch(r0, xl, xh, yl, yh);
+      first();
+      for (int r = r0; r < r1; ++r) {
+        if (r + 1 < r1) fetch(r + 1, xl2, xh2, yl2, yh2);
+        float ss = 0.f, dot = 0.f, d0[8], d1[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          d0[j] = yl.at(j) * l.cs[j] + yh.at(j) * l.sn[j];
+          d1[j] = yh.at(j) * l.cs[j] - yl.at(j) * l.sn[j];
+          ss = fmaf(xl.at(j), xl.at(j), fmaf(xh.at(j), xh.at(j), ss));
+          dot = fmaf(d0[j] * g[j], xl.at(j), fmaf(d1[j] * g[8 + j], xh.at(j), dot));
+        }
+        const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
+        const float k3 = rs * rs * rs * (group_sum<G>(dot) / (float)a.d);
+        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
+        if (l.used && h < heads) {
+          float p[8], q[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p[j] = rs * (g[j] * d0[j]) - k3 * xl.at(j);
+            q[j] = rs * (g[8 + j] * d1[j]) - k3 * xh.at(j);
+            dg[j] = fmaf(d0[j] * xl.at(j), rs, dg[j]);
+            dg[8 + j] = fmaf(d1[j] * xh.at(j), rs, dg[8 + j]);
+          }
+          Chunk<T>::store(dx + (long)h * a.d + l.col, p);
+          Chunk<T>::store(dx + (long)h * a.d + l.col + l.half, q);
+        }
+        xl = xl2;
+        xh = xh2;
+        yl = yl2;
+        yh = yh2;
+      }
+    };
+    bool formed = false;
+    auto angles = [&] {
+      if (!formed) l.angles(a, t, shared[w]);
+      formed = true;
+    };
+    sweep(n.q0, n.q1, (const T*)a.q + t * a.q_stride, (const T*)a.dyq + t * a.hq * a.d, (T*)a.dq + t * a.dq_stride,
+          a.hq, gq, dgq, angles);
+    sweep(n.k0, n.k1, (const T*)a.k + t * a.k_stride, (const T*)a.dyk + t * a.hkv * a.d, (T*)a.dk + t * a.dk_stride,
+          a.hkv, gk, dgk, angles);
+  }
+  // gain gradients: over the wave's heads, then over the workgroup's waves
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+#pragma unroll
+    for (int o = G; o < 64; o <<= 1) {
+      dgq[j] += __shfl_xor(dgq[j], o);
+      dgk[j] += __shfl_xor(dgk[j], o);
+    }
+    if (l.lane < G && l.used) {
+      const int col = l.col + j % 8 + (j < 8 ? 0 : l.half);
+      red[w][0][col] = dgq[j];
+      red[w][1][col] = dgk[j];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * a.d; i += kHeadThreads) {
+    float sum = 0.f;
+    for (int q = 0; q < kHeadWaves; ++q) sum += red[q][i / a.d][i % a.d];
+    a.part[(long)blockIdx.x * 2 * a.d + i] = sum;
+  }
+}
+
+// dgain (+)= the sum of part over its blocks: 16 columns of the 2 d a workgroup,
+// 64 interleaved slices of the blocks, added in a fixed order
 __global__ __launch_bounds__(1024) void head_gain_sum_kernel(const float* __restrict__ part, int blocks, int d,
                                                              float* __restrict__ dgq, float* __restrict__ dgk,
                                                              int overwrite) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
+  __shared__ float red[64][17];
+  const int c = threadIdx.x & 15, s = threadIdx.x >> 4, i = blockIdx.x * 16 + c;
   float sum = 0.f;
   if (i < 2 * d)
-    for (int b = w; b < blocks; b += 16) sum += part[(long)b * 2 * d + i];
-  red[w][lane] = sum;
+#pragma unroll 8
+    for (int b = s; b < blocks; b += 64) sum += part[(long)b * 2 * d + i];
+  red[s][c] = sum;
   __syncthreads();
-  if (w != 0 || i >= 2 * d) return;
-  sum = 0.f;
-  for (int q = 0; q < 16; ++q) sum += red[q][lane];
+  for (int o = 32; o > 0; o >>= 1) {
+    if (s < o) red[s][c] += red[s + o][c];
+    __syncthreads();
+  }
+  if (s != 0 || i >= 2 * d) return;
   float* dst = i < d ? dgq + i : dgk + i - d;
-  *dst = overwrite ? sum : *dst + sum;
+  *dst = overwrite ? red[0][c] : *dst + red[0][c];
 }
 
 namespace {
-// workgroups of the backward: four waves each, a row a wave at least, and
-// enough of them to fill the chip eight waves deep per SIMD
-constexpr long kHeadBwdBlocks = 2048;
+// Workgroups of the backward, whose gain-gradient partials the workspace holds:
+// four waves each, a row a wave at least.
+constexpr long kHeadBwdBlocks = 1024;
 long head_bwd_blocks(long rows) { return std::max(1L, std::min(kHeadBwdBlocks, (rows + kHeadWaves - 1) / kHeadWaves)); }
+
+// 16-byte chunks everywhere: what the row kernels read and write as such
+bool by_chunks(const HeadArgs& a, int es) {
+  const uintptr_t bits = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.dq | (uintptr_t)a.dk |
+                         (uintptr_t)((a.q_stride | a.k_stride | a.dq_stride | a.dk_stride) * es);
+  return a.d % 16 == 0 && bits % 16 == 0;
+}
+// lanes of a row: a power of two that holds d / 16 chunk pairs
+int row_lanes(int d) {
+  int g = 1;
+  while (16 * g < d) g *= 2;
+  return g;
+}
+// Shares of a token's heads: one while there are waves enough (four thousand,
+// four a SIMD), else up to one per round of heads, so that a few tokens still
+// use the chip.
+int head_parts(const HeadArgs& a) {
+  const int heads = 64 / row_lanes(a.d);
+  const int rounds = (a.hq + heads - 1) / heads + (a.hkv + heads - 1) / heads;
+  const long want = a.tokens > 0 ? 4096 / a.tokens : 1;
+  return (int)std::max(1L, std::min((long)rounds, want));
+}
+
+// the instantiation for the head dim's lanes per row
+template <typename T, bool BWD>
+void launch_rows(const HeadArgs& a, unsigned blocks, int parts, hipStream_t st) {
+#define SPR_ROWS(G)                                                                                              \
+  case G:                                                                                                        \
+    if (BWD)                                                                                                     \
+      hipLaunchKernelGGL((head_rows_bwd_kernel<T, G>), dim3(blocks), dim3(kHeadThreads), 0, st, a, parts);       \
+    else                                                                                                         \
+      hipLaunchKernelGGL((head_rows_fwd_kernel<T, G>), dim3(blocks), dim3(kHeadThreads), 0, st, a, parts);       \
+    break
+  switch (row_lanes(a.d)) {
+    SPR_ROWS(1);
+    SPR_ROWS(2);
+    SPR_ROWS(4);
+    SPR_ROWS(8);
+    SPR_ROWS(16);
+  }
+#undef SPR_ROWS
+}
 }  // namespace
 
 size_t head_norm_rope_bwd_ws(long rows, int d) { return (size_t)head_bwd_blocks(rows) * 2 * d * 4; }
@@ -177,6 +488,15 @@ hipError_t launch_head_norm_rope_fwd(int dtype, const HeadArgs& a, hipStream_t s
   const long rows = (long)a.tokens * (a.hq + a.hkv);
   if (rows == 0) return hipSuccess;
   ProfileScope ps("head_norm_rope_fwd", st);
+  if (by_chunks(a, dtype == 1 ? 2 : 4)) {
+    const int parts = head_parts(a);
+    const long units = (long)a.tokens * parts, blocks = std::min(2048L, (units + kHeadWaves - 1) / kHeadWaves);
+    if (dtype == 1)
+      launch_rows<bf16, false>(a, (unsigned)blocks, parts, st);
+    else
+      launch_rows<float, false>(a, (unsigned)blocks, parts, st);
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)((rows + kHeadWaves - 1) / kHeadWaves));
   if (dtype == 1)
     hipLaunchKernelGGL(head_norm_rope_fwd_kernel<bf16>, grid, dim3(kHeadThreads), 0, st, a);
@@ -189,16 +509,25 @@ hipError_t launch_head_norm_rope_bwd(int dtype, const HeadArgs& a, float* dgain_
                                      hipStream_t st) {
   const long rows = (long)a.tokens * (a.hq + a.hkv);
   if (rows == 0 && !overwrite) return hipSuccess;
-  const unsigned blocks = (unsigned)head_bwd_blocks(rows);
-  {
+  long blocks = rows > 0 ? head_bwd_blocks(rows) : 0;  // no tokens: the gains' gradient is zero
+  if (rows > 0) {
     ProfileScope ps("head_norm_rope_bwd", st);
-    if (dtype == 1)
-      hipLaunchKernelGGL(head_norm_rope_bwd_kernel<bf16>, dim3(blocks), dim3(kHeadThreads), 0, st, a);
-    else
-      hipLaunchKernelGGL(head_norm_rope_bwd_kernel<float>, dim3(blocks), dim3(kHeadThreads), 0, st, a);
+    if (by_chunks(a, dtype == 1 ? 2 : 4)) {
+      const int parts = head_parts(a);
+      // never more waves than units: an idle wave's partial would be read for nothing
+      blocks = std::max(1L, std::min(blocks, ((long)a.tokens * parts + kHeadWaves - 1) / kHeadWaves));
+      if (dtype == 1)
+        launch_rows<bf16, true>(a, (unsigned)blocks, parts, st);
+      else
+        launch_rows<float, true>(a, (unsigned)blocks, parts, st);
+    } else if (dtype == 1) {
+      hipLaunchKernelGGL(head_norm_rope_bwd_kernel<bf16>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, st, a);
+    } else {
+      hipLaunchKernelGGL(head_norm_rope_bwd_kernel<float>, dim3((unsigned)blocks), dim3(kHeadThreads), 0, st, a);
+    }
   }
   ProfileScope ps("head_gain_sum", st);
-  hipLaunchKernelGGL(head_gain_sum_kernel, dim3((2 * a.d + 63) / 64), dim3(1024), 0, st, a.part, (int)blocks, a.d,
+  hipLaunchKernelGGL(head_gain_sum_kernel, dim3((2 * a.d + 15) / 16), dim3(1024), 0, st, a.part, (int)blocks, a.d,
                      dgain_q, dgain_k, overwrite ? 1 : 0);
   return hipGetLastError();
 }
