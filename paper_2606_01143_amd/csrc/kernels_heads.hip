@@ -236,25 +236,59 @@ struct RowLane {
       sn[j] = v.y;
     }
   }
-  // gain values of the chunk: [0, 8) of the lower half, [8, 16) of the upper
-  __device__ __forceinline__ void gains(const T* g, float (&out)[16]) const {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      out[j] = used ? to_f32(g[col + j]) : 0.f;
-      out[8 + j] = used ? to_f32(g[col + half + j]) : 0.f;
+};
+
+// both halves' chunks of a row
+template <typename T>
+struct Pair {
+  Chunk<T> lo, hi;
+  __device__ __forceinline__ void load(const T* row, int col, int half, bool used) {
+    lo.zero();
+    hi.zero();
+    if (used) {
+      lo.load(row + col);
+      hi.load(row + col + half);
     }
   }
 };
 
-// rounds of `heads` heads, kHeads at a time, that share `part` of `parts` takes
-// of q's and k's rounds together
-struct Rounds {
-  int q0, q1, k0, k1;
+// A token's heads in rounds of 64 / G, q's before k's; a unit is a token's share
+// [part * per, ..) of them.  A wave's units lie `stride` apart, and it walks
+// their rounds as one sequence.
+struct Cursor {
+  long u;
+  int r;
 };
-__device__ __forceinline__ Rounds rounds_of(const HeadArgs& a, int heads, int part, int parts) {
-  const int nq = (a.hq + heads - 1) / heads, n = nq + (a.hkv + heads - 1) / heads, per = (n + parts - 1) / parts;
-  const int lo = min(part * per, n), hi = min(lo + per, n);
-  return {min(lo, nq), min(hi, nq), max(lo, nq) - nq, max(hi, nq) - nq};
+template <int G>
+struct Walk {
+  int nq, n, per, parts;
+  long units, stride;
+  __device__ __forceinline__ Walk(const HeadArgs& a, int parts_) {
+    constexpr int H = 64 / G;
+    nq = (a.hq + H - 1) / H;
+    n = nq + (a.hkv + H - 1) / H;
+    parts = parts_;
+    per = (n + parts - 1) / parts;
+    units = (long)a.tokens * parts;
+    stride = (long)gridDim.x * kHeadWaves;
+  }
+  __device__ __forceinline__ int lo(long u) const { return (int)(u % parts) * per; }
+  __device__ __forceinline__ bool ends(const Cursor& c) const { return c.u >= units; }
+  __device__ __forceinline__ Cursor after(const Cursor& c) const {
+    if (c.r + 1 < min(lo(c.u) + per, n)) return {c.u, c.r + 1};
+    return {c.u + stride, lo(c.u + stride)};
+  }
+};
+// the rows of a cursor's round: heads of q or of k
+struct Round {
+  bool is_q;
+  long t;
+  int first, heads;
+};
+template <int G>
+__device__ __forceinline__ Round round_at(const HeadArgs& a, const Walk<G>& w, const Cursor& c) {
+  const bool is_q = c.r < w.nq;
+  return {is_q, c.u / w.parts, (is_q ? c.r : c.r - w.nq) * (64 / G), is_q ? a.hq : a.hkv};
 }
 }  // namespace
 
@@ -262,57 +296,50 @@ template <typename T, int G>
 __global__ __launch_bounds__(kHeadThreads) void head_rows_fwd_kernel(HeadArgs a, int parts) {
   __shared__ float2 shared[kHeadWaves][64 * kMaxPairs];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Walk<G> walk(a, parts);
+  Cursor cur = {(long)blockIdx.x * kHeadWaves + w, 0};
+  if (walk.ends(cur)) return;
+  cur.r = walk.lo(cur.u);
+  const int lane = threadIdx.x & 63, half = a.d / 2, col = lane % G * 8;
+  auto fetch = [&](const Cursor& c, Pair<T>& x) {
+    const Round r = round_at<G>(a, walk, c);
+    const int h = r.first + lane / G;
+    const T* token = r.is_q ? (const T*)a.q + r.t * a.q_stride : (const T*)a.k + r.t * a.k_stride;
+    x.load(token + h * a.d, col, half, col < half && h < r.heads);
+  };
+  Pair<T> x, ahead, gq, gk;
+  fetch(cur, x);
+  gq.load((const T*)a.gain_q, col, half, col < half);
+  gk.load((const T*)a.gain_k, col, half, col < half);
   RowLane<T, G> l(a);
-  float gq[16], gk[16];
-  l.gains((const T*)a.gain_q, gq);
-  l.gains((const T*)a.gain_k, gk);
-  const long units = (long)a.tokens * parts, stride = (long)gridDim.x * kHeadWaves;
-  for (long u = (long)blockIdx.x * kHeadWaves + w; u < units; u += stride) {
-    const long t = u / parts;
-    const Rounds n = rounds_of(a, RowLane<T, G>::kHeads, (int)(u % parts), parts);
-    auto sweep = [&](int r0, int r1, const T* x, T* y, int heads, const float (&g)[16], auto&& first) {
-      Chunk<T> lo, hi, lo2, hi2;
-      auto fetch = [&](int r, Chunk<T>& p, Chunk<T>& q) {
-        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
-        p.zero();
-        q.zero();
-        if (l.used && h < heads) {
-          p.load(x + (long)h * a.d + l.col);
-          q.load(x + (long)h * a.d + l.col + l.half);
-        }
-      };
-      if (r0 < r1) fetch(r0, lo, hi);
-      first();
-      for (int r = r0; r < r1; ++r) {
-        if (r + 1 < r1) fetch(r + 1, lo2, hi2);
-        float ss = 0.f;
+  for (bool begins = true;;) {
+    const Cursor next = walk.after(cur);
+    const bool more = !walk.ends(next);
+    if (more) fetch(next, ahead);
+    const Round r = round_at<G>(a, walk, cur);
+    if (begins) l.angles(a, r.t, shared[w]);
+    float ss = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ss = fmaf(lo.at(j), lo.at(j), fmaf(hi.at(j), hi.at(j), ss));
-        const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
-        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
-        if (l.used && h < heads) {
-          float p[8], q[8];
+    for (int j = 0; j < 8; ++j) ss = fmaf(x.lo.at(j), x.lo.at(j), fmaf(x.hi.at(j), x.hi.at(j), ss));
+    const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
+    const int h = r.first + lane / G;
+    if (col < half && h < r.heads) {
+      const Pair<T>& g = r.is_q ? gq : gk;
+      T* y = (r.is_q ? (T*)a.yq : (T*)a.yk) + (r.t * r.heads + h) * a.d + col;
+      float p[8], q[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float u0 = lo.at(j) * rs * g[j], u1 = hi.at(j) * rs * g[8 + j];
-            p[j] = u0 * l.cs[j] - u1 * l.sn[j];
-            q[j] = u1 * l.cs[j] + u0 * l.sn[j];
-          }
-          Chunk<T>::store(y + (long)h * a.d + l.col, p);
-          Chunk<T>::store(y + (long)h * a.d + l.col + l.half, q);
-        }
-        lo = lo2;
-        hi = hi2;
+      for (int j = 0; j < 8; ++j) {
+        const float u0 = x.lo.at(j) * rs * g.lo.at(j), u1 = x.hi.at(j) * rs * g.hi.at(j);
+        p[j] = u0 * l.cs[j] - u1 * l.sn[j];
+        q[j] = u1 * l.cs[j] + u0 * l.sn[j];
       }
-    };
-    // the first rows are on their way while the angles are formed
-    bool formed = false;
-    auto angles = [&] {
-      if (!formed) l.angles(a, t, shared[w]);
-      formed = true;
-    };
-    sweep(n.q0, n.q1, (const T*)a.q + t * a.q_stride, (T*)a.yq + t * a.hq * a.d, a.hq, gq, angles);
-    sweep(n.k0, n.k1, (const T*)a.k + t * a.k_stride, (T*)a.yk + t * a.hkv * a.d, a.hkv, gk, angles);
+      Chunk<T>::store(y, p);
+      Chunk<T>::store(y + half, q);
+    }
+    if (!more) break;
+    begins = next.u != cur.u;
+    x = ahead;
+    cur = next;
   }
 }
 
@@ -321,73 +348,69 @@ __global__ __launch_bounds__(kHeadThreads) void head_rows_bwd_kernel(HeadArgs a,
   __shared__ float2 shared[kHeadWaves][64 * kMaxPairs];
   __shared__ float red[kHeadWaves][2][2 * 64 * kMaxPairs];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Walk<G> walk(a, parts);
+  Cursor cur = {(long)blockIdx.x * kHeadWaves + w, 0};
+  cur.r = walk.lo(cur.u);
+  const int lane = threadIdx.x & 63, half = a.d / 2, col = lane % G * 8;
+  auto fetch = [&](const Cursor& c, Pair<T>& x, Pair<T>& y) {
+    const Round r = round_at<G>(a, walk, c);
+    const int h = r.first + lane / G;
+    const bool used = col < half && h < r.heads;
+    const T* token = r.is_q ? (const T*)a.q + r.t * a.q_stride : (const T*)a.k + r.t * a.k_stride;
+    x.load(token + h * a.d, col, half, used);
+    y.load((r.is_q ? (const T*)a.dyq : (const T*)a.dyk) + (r.t * r.heads + h) * a.d, col, half, used);
+  };
+  Pair<T> x, y, ahead_x, ahead_y, gq, gk;
+  bool more = !walk.ends(cur);
+  if (more) fetch(cur, x, y);
+  gq.load((const T*)a.gain_q, col, half, col < half);
+  gk.load((const T*)a.gain_k, col, half, col < half);
   RowLane<T, G> l(a);
-  float gq[16], gk[16], dgq[16] = {}, dgk[16] = {};
-  l.gains((const T*)a.gain_q, gq);
-  l.gains((const T*)a.gain_k, gk);
-  const long units = (long)a.tokens * parts, stride = (long)gridDim.x * kHeadWaves;
-  for (long u = (long)blockIdx.x * kHeadWaves + w; u < units; u += stride) {
-    const long t = u / parts;
-    const Rounds n = rounds_of(a, RowLane<T, G>::kHeads, (int)(u % parts), parts);
-    auto sweep = [&](int r0, int r1, const T* x, const T* dy, T* dx, int heads, const float (&g)[16], float (&dg)[16],
-                     auto&& first) {
-      Chunk<T> xl, xh, yl, yh, xl2, xh2, yl2, yh2;
-      auto fetch = [&](int r, Chunk<T>& p, Chunk<T>& q, Chunk<T>& e, Chunk<T>& f) {
-        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
-        p.zero();
-        q.zero();
-        e.zero();
-        f.zero();
-        if (l.used && h < heads) {
-          const long at = (long)h * a.d + l.col;
-          p.load(x + at);
-          q.load(x + at + l.half);
-          e.load(dy + at);
-          f.load(dy + at + l.half);
-        }
-      };
-      if (r0 < r1) fetch(r0, xl, xh, yl, yh);
-      first();
-      for (int r = r0; r < r1; ++r) {
-        if (r + 1 < r1) fetch(r + 1, xl2, xh2, yl2, yh2);
-        float ss = 0.f, dot = 0.f, d0[8], d1[8];
+  float dgq[16] = {}, dgk[16] = {};
+  for (bool begins = true; more;) {
+    const Cursor next = walk.after(cur);
+    more = !walk.ends(next);
+    if (more) fetch(next, ahead_x, ahead_y);
+    const Round r = round_at<G>(a, walk, cur);
+    if (begins) l.angles(a, r.t, shared[w]);
+    const Pair<T>& g = r.is_q ? gq : gk;
+    float ss = 0.f, dot = 0.f, d0[8], d1[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      d0[j] = y.lo.at(j) * l.cs[j] + y.hi.at(j) * l.sn[j];
+      d1[j] = y.hi.at(j) * l.cs[j] - y.lo.at(j) * l.sn[j];
+      ss = fmaf(x.lo.at(j), x.lo.at(j), fmaf(x.hi.at(j), x.hi.at(j), ss));
+      dot = fmaf(d0[j] * g.lo.at(j), x.lo.at(j), fmaf(d1[j] * g.hi.at(j), x.hi.at(j), dot));
+    }
+    const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
+    const float k3 = rs * rs * rs * (group_sum<G>(dot) / (float)a.d);
+    const int h = r.first + lane / G;
+    if (col < half && h < r.heads) {
+      T* dx = (r.is_q ? (T*)a.dq + r.t * a.dq_stride : (T*)a.dk + r.t * a.dk_stride) + h * a.d + col;
+      float p[8], q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        p[j] = rs * (g.lo.at(j) * d0[j]) - k3 * x.lo.at(j);
+        q[j] = rs * (g.hi.at(j) * d1[j]) - k3 * x.hi.at(j);
+      }
+      Chunk<T>::store(dx, p);
+      Chunk<T>::store(dx + half, q);
+      auto add = [&](float (&dg)[16]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          d0[j] = yl.at(j) * l.cs[j] + yh.at(j) * l.sn[j];
-          d1[j] = yh.at(j) * l.cs[j] - yl.at(j) * l.sn[j];
-          ss = fmaf(xl.at(j), xl.at(j), fmaf(xh.at(j), xh.at(j), ss));
-          dot = fmaf(d0[j] * g[j], xl.at(j), fmaf(d1[j] * g[8 + j], xh.at(j), dot));
+          dg[j] = fmaf(d0[j] * x.lo.at(j), rs, dg[j]);
+          dg[8 + j] = fmaf(d1[j] * x.hi.at(j), rs, dg[8 + j]);
         }
-        const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
-        const float k3 = rs * rs * rs * (group_sum<G>(dot) / (float)a.d);
-        const int h = r * RowLane<T, G>::kHeads + l.lane / G;
-        if (l.used && h < heads) {
-          float p[8], q[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            p[j] = rs * (g[j] * d0[j]) - k3 * xl.at(j);
-            q[j] = rs * (g[8 + j] * d1[j]) - k3 * xh.at(j);
-            dg[j] = fmaf(d0[j] * xl.at(j), rs, dg[j]);
-            dg[8 + j] = fmaf(d1[j] * xh.at(j), rs, dg[8 + j]);
-          }
-          Chunk<T>::store(dx + (long)h * a.d + l.col, p);
-          Chunk<T>::store(dx + (long)h * a.d + l.col + l.half, q);
-        }
-        xl = xl2;
-        xh = xh2;
-        yl = yl2;
-        yh = yh2;
-      }
-    };
-    bool formed = false;
-    auto angles = [&] {
-      if (!formed) l.angles(a, t, shared[w]);
-      formed = true;
-    };
-    sweep(n.q0, n.q1, (const T*)a.q + t * a.q_stride, (const T*)a.dyq + t * a.hq * a.d, (T*)a.dq + t * a.dq_stride,
-          a.hq, gq, dgq, angles);
-    sweep(n.k0, n.k1, (const T*)a.k + t * a.k_stride, (const T*)a.dyk + t * a.hkv * a.d, (T*)a.dk + t * a.dk_stride,
-          a.hkv, gk, dgk, angles);
+      };
+      if (r.is_q)
+        add(dgq);
+      else
+        add(dgk);
+    }
+    begins = next.u != cur.u;
+    x = ahead_x;
+    y = ahead_y;
+    cur = next;
   }
   // gain gradients: over the wave's heads, then over the workgroup's waves
 #pragma unroll
@@ -397,10 +420,9 @@ __global__ __launch_bounds__(kHeadThreads) void head_rows_bwd_kernel(HeadArgs a,
       dgq[j] += __shfl_xor(dgq[j], o);
       dgk[j] += __shfl_xor(dgk[j], o);
     }
-    if (l.lane < G && l.used) {
-      const int col = l.col + j % 8 + (j < 8 ? 0 : l.half);
-      red[w][0][col] = dgq[j];
-      red[w][1][col] = dgk[j];
+    if (lane < G && col < half) {
+      red[w][0][col + j % 8 + (j < 8 ? 0 : half)] = dgq[j];
+      red[w][1][col + j % 8 + (j < 8 ? 0 : half)] = dgk[j];
     }
   }
   __syncthreads();
@@ -442,6 +464,7 @@ long head_bwd_blocks(long rows) { return std::max(1L, std::min(kHeadBwdBlocks, (
 // 16-byte chunks everywhere: what the row kernels read and write as such
 bool by_chunks(const HeadArgs& a, int es) {
   const uintptr_t bits = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.dq | (uintptr_t)a.dk |
+                         (uintptr_t)a.gain_q | (uintptr_t)a.gain_k |
                          (uintptr_t)((a.q_stride | a.k_stride | a.dq_stride | a.dk_stride) * es);
   return a.d % 16 == 0 && bits % 16 == 0;
 }
@@ -458,7 +481,8 @@ int head_parts(const HeadArgs& a) {
   const int heads = 64 / row_lanes(a.d);
   const int rounds = (a.hq + heads - 1) / heads + (a.hkv + heads - 1) / heads;
   const long want = a.tokens > 0 ? 4096 / a.tokens : 1;
-  return (int)std::max(1L, std::min((long)rounds, want));
+  const int parts = (int)std::max(1L, std::min((long)rounds, want)), per = (rounds + parts - 1) / parts;
+  return (rounds + per - 1) / per;  // no empty share
 }
 
 // the instantiation for the head dim's lanes per row
@@ -490,7 +514,7 @@ hipError_t launch_head_norm_rope_fwd(int dtype, const HeadArgs& a, hipStream_t s
   ProfileScope ps("head_norm_rope_fwd", st);
   if (by_chunks(a, dtype == 1 ? 2 : 4)) {
     const int parts = head_parts(a);
-    const long units = (long)a.tokens * parts, blocks = std::min(2048L, (units + kHeadWaves - 1) / kHeadWaves);
+    const long units = (long)a.tokens * parts, blocks = std::min(1024L, (units + kHeadWaves - 1) / kHeadWaves);
     if (dtype == 1)
       launch_rows<bf16, false>(a, (unsigned)blocks, parts, st);
     else
