@@ -422,48 +422,76 @@ def rope_bwd(dy, dx, pos0, theta, stream=None):
     _check(lib().spr_rope_bwd(t, h, d, pos0, float(theta), _ptr(dy), _ptr(dx), _stream(stream)))
 
 
-def _typed(dtype, **tensors):
-    """Every named tensor has elements of torch dtype ``dtype`` (fp16 has bf16's
-    size and is refused here) and lies on the current device, whose stream the
-    call takes; None is left to the library."""
-    import torch
-    for name, x in tensors.items():
-        if x is None:
-            continue
-        if x.dtype != dtype:
-            raise ValueError(f"{name}: {x.dtype}, the call needs {dtype}")
-        if x.is_cuda and x.device.index != torch.cuda.current_device():
-            raise ValueError(f"{name} is on {x.device}, not on the current device "
-                             f"cuda:{torch.cuda.current_device()}")
+def _refuse(name, x, dtype, shape, dev):
+    """Why _arg turned a tensor away."""
+    if x.dtype is not dtype:
+        raise ValueError(f"{name}: {x.dtype}, the call needs {dtype}")
+    if shape is not None and x.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(x.shape)}, the call needs {tuple(shape)}")
+    if not x.is_cuda:
+        raise ValueError("libspr takes GPU tensors only")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} is on cuda:{x.get_device()}, not on the call's device cuda:{dev}")
+    raise ValueError("libspr takes contiguous tensors only")
+
+
+def _arg(name, x, dtype, shape, dev):
+    """Pointer of a contiguous tensor of that type and shape on device ``dev``
+    (the type exactly: fp16 has bf16's size); None is left to the library."""
+    if x is None:
+        return None
+    if x.dtype is dtype and x.shape == shape and x.get_device() == dev and x.is_contiguous():
+        return x.data_ptr()
+    _refuse(name, x, dtype, shape, dev)
+
+
+def _rows_arg(name, x, dtype, shape, dev):
+    """Pointer and token stride of [tokens, heads, d] whose heads and values
+    are contiguous (a view of a fused projection)."""
+    if x.dtype is not dtype or x.shape != shape or x.get_device() != dev:
+        _refuse(name, x, dtype, shape, dev)
+    t, h, d = shape
+    s0, s1, s2 = x.stride()
+    if (d > 1 and s2 != 1) or (h > 1 and s1 != d):
+        raise ValueError(f"{name}: a token's heads are not contiguous")
+    if t <= 1:
+        return x.data_ptr(), h * d
+    if s0 < h * d:
+        raise ValueError(f"{name}: tokens overlap (stride {s0}, a token has {h * d} elements)")
+    return x.data_ptr(), s0
+
+
+def _ws(ws, dev):
+    """Pointer and bytes of a workspace (None: a NULL pointer)."""
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        _refuse("ws", ws, ws.dtype, None, dev)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _storage(name, x):
     """The library's dtype code of a tensor that may be bf16 or fp32."""
     import torch
-    code = {torch.bfloat16: SPR_BF16, torch.float32: SPR_F32}.get(x.dtype)
-    if code is None:
-        raise ValueError(f"{name}: {x.dtype}, the call takes bfloat16 or float32")
-    return code
+    if x.dtype is torch.bfloat16:
+        return SPR_BF16
+    if x.dtype is torch.float32:
+        return SPR_F32
+    raise ValueError(f"{name}: {x.dtype}, the call takes bfloat16 or float32")
 
 
-def _shaped(shape, **tensors):
-    for name, x in tensors.items():
-        if x is not None and tuple(x.shape) != tuple(shape):
-            raise ValueError(f"{name}: shape {tuple(x.shape)}, the call needs {tuple(shape)}")
-
-
-def _token_rows(name, x):
-    """Pointer and token stride of [tokens, heads, d] whose heads and values
-    are contiguous (a view of a fused projection)."""
-    t, h, d = (int(v) for v in x.shape)
-    if not x.is_cuda:
+def _on(dev, stream):
+    """The stream of a call whose tensors lie on ``dev``: it has to be the
+    current device, whose stream is taken where none is given."""
+    import torch
+    if dev < 0:
         raise ValueError("libspr takes GPU tensors only")
-    if (d > 1 and x.stride(2) != 1) or (h > 1 and x.stride(1) != d):
-        raise ValueError(f"{name}: a token's heads are not contiguous")
-    stride = int(x.stride(0)) if t > 1 else h * d
-    if stride < h * d:
-        raise ValueError(f"{name}: tokens overlap (stride {stride}, a token has {h * d} elements)")
-    return x.data_ptr(), stride
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{dev}, not on the current device "
+                         f"cuda:{torch.cuda.current_device()}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def head_norm_rope_bwd_workspace_size(tokens, q_heads, kv_heads, head_dim) -> int:
@@ -478,17 +506,15 @@ def head_norm_rope_fwd(q, k, gain_q, gain_k, yq, yk, pos0, theta, positions=None
     projection (heads contiguous).  ``positions``: int32 [T], added to pos0 in
     place of 0 .. T - 1."""
     import torch
-    (t, hq, d), hkv = (int(v) for v in q.shape), int(k.shape[1])
-    code = _storage("q", q)
-    _typed(q.dtype, q=q, k=k, gain_q=gain_q, gain_k=gain_k, yq=yq, yk=yk)
-    _typed(torch.int32, positions=positions)
-    _shaped((t, hq, d), yq=yq)
-    _shaped((t, hkv, d), k=k, yk=yk)
-    _shaped((d,), gain_q=gain_q, gain_k=gain_k)
-    _shaped((t,), positions=positions)
-    (pq, sq), (pk, sk) = _token_rows("q", q), _token_rows("k", k)
-    _check(lib().spr_head_norm_rope_fwd(code, t, hq, hkv, d, eps, pos0, _ptr(positions), float(theta), pq, sq, pk, sk,
-                                        _ptr(gain_q), _ptr(gain_k), _ptr(yq), _ptr(yk), _stream(stream)))
+    sq, (t, hkv, d), dt, dev = q.shape, k.shape, q.dtype, q.get_device()
+    code, hq, sk = _storage("q", q), sq[1], (sq[0], hkv, sq[2])
+    pq, stride_q = _rows_arg("q", q, dt, sq, dev)
+    pk, stride_k = _rows_arg("k", k, dt, sk, dev)
+    args = (_arg("gain_q", gain_q, dt, (d,), dev), _arg("gain_k", gain_k, dt, (d,), dev), _arg("yq", yq, dt, sq, dev),
+            _arg("yk", yk, dt, sk, dev))
+    _check(lib().spr_head_norm_rope_fwd(code, t, hq, hkv, d, float(eps), pos0,
+                                        _arg("positions", positions, torch.int32, (t,), dev), float(theta), pq, stride_q, pk,
+                                        stride_k, *args, _on(dev, stream)))
 
 
 def head_norm_rope_bwd(q, k, gain_q, gain_k, dyq, dyk, dq, dk, dgain_q, dgain_k, pos0, theta, positions=None,
@@ -497,32 +523,28 @@ def head_norm_rope_bwd(q, k, gain_q, gain_k, dyq, dyk, dq, dk, dgain_q, dgain_k,
     one fused gradient) are written, dgain_q and dgain_k [d] fp32 added to, or
     written where ``overwrite``."""
     import torch
-    (t, hq, d), hkv = (int(v) for v in q.shape), int(k.shape[1])
-    code = _storage("q", q)
-    _typed(q.dtype, q=q, k=k, gain_q=gain_q, gain_k=gain_k, dyq=dyq, dyk=dyk, dq=dq, dk=dk)
-    _typed(torch.int32, positions=positions)
-    _typed(torch.float32, dgain_q=dgain_q, dgain_k=dgain_k)
-    _shaped((t, hq, d), dyq=dyq, dq=dq)
-    _shaped((t, hkv, d), k=k, dyk=dyk, dk=dk)
-    _shaped((d,), gain_q=gain_q, gain_k=gain_k, dgain_q=dgain_q, dgain_k=dgain_k)
-    _shaped((t,), positions=positions)
-    (pq, sq), (pk, sk) = _token_rows("q", q), _token_rows("k", k)
-    (pdq, sdq), (pdk, sdk) = _token_rows("dq", dq), _token_rows("dk", dk)
-    _check(lib().spr_head_norm_rope_bwd(code, t, hq, hkv, d, eps, pos0, _ptr(positions), float(theta), pq, sq, pk, sk,
-                                        _ptr(gain_q), _ptr(gain_k), _ptr(dyq), _ptr(dyk), pdq, sdq, pdk, sdk,
-                                        _ptr(dgain_q), _ptr(dgain_k), 1 if overwrite else 0, _ptr(ws), _nbytes(ws),
-                                        _stream(stream)))
+    sq, (t, hkv, d), dt, dev = q.shape, k.shape, q.dtype, q.get_device()
+    code, hq, sk, f32 = _storage("q", q), sq[1], (sq[0], hkv, sq[2]), torch.float32
+    pq, stride_q = _rows_arg("q", q, dt, sq, dev)
+    pk, stride_k = _rows_arg("k", k, dt, sk, dev)
+    ins = (_arg("gain_q", gain_q, dt, (d,), dev), _arg("gain_k", gain_k, dt, (d,), dev),
+           _arg("dyq", dyq, dt, sq, dev), _arg("dyk", dyk, dt, sk, dev))
+    outs = (*_rows_arg("dq", dq, dt, sq, dev), *_rows_arg("dk", dk, dt, sk, dev),
+            _arg("dgain_q", dgain_q, f32, (d,), dev), _arg("dgain_k", dgain_k, f32, (d,), dev))
+    _check(lib().spr_head_norm_rope_bwd(code, t, hq, hkv, d, float(eps), pos0,
+                                        _arg("positions", positions, torch.int32, (t,), dev), float(theta), pq, stride_q, pk,
+                                        stride_k, *ins, *outs, 1 if overwrite else 0, *_ws(ws, dev),
+                                        _on(dev, stream)))
 
 
 def embed_fwd(ids, table, y, scale=1.0, stream=None):
     """y[t] = scale * table[ids[t]]; an id outside the table gives zeros."""
     import torch
-    (t,), (v, w) = ids.shape, table.shape
+    (t,), (v, w), dt, dev = ids.shape, table.shape, table.dtype, table.get_device()
     code = _storage("table", table)
-    _typed(torch.int32, ids=ids)
-    _typed(table.dtype, table=table, y=y)
-    _shaped((t, w), y=y)
-    _check(lib().spr_embed_fwd(code, t, v, w, float(scale), _ptr(ids), _ptr(table), _ptr(y), _stream(stream)))
+    _check(lib().spr_embed_fwd(code, t, v, w, float(scale), _arg("ids", ids, torch.int32, (t,), dev),
+                               _arg("table", table, dt, (v, w), dev), _arg("y", y, dt, (t, w), dev),
+                               _on(dev, stream)))
 
 
 def embed_bwd_workspace_size(tokens, vocab, width) -> int:
@@ -534,14 +556,12 @@ def embed_bwd_workspace_size(tokens, vocab, width) -> int:
 def embed_bwd(ids, dy, dtable, scale=1.0, ws=None, stream=None):
     """dtable[v] += scale * the sum of dy over v's tokens, fp32, in token order."""
     import torch
-    (t,), (v, w) = ids.shape, dtable.shape
+    (t,), (v, w), dev = ids.shape, dtable.shape, dtable.get_device()
     code = _storage("dy", dy)
-    _typed(torch.int32, ids=ids)
-    _typed(dy.dtype, dy=dy)
-    _typed(torch.float32, dtable=dtable)
-    _shaped((t, w), dy=dy)
-    _check(lib().spr_embed_bwd(code, t, v, w, float(scale), _ptr(ids), _ptr(dy), _ptr(dtable), _ptr(ws), _nbytes(ws),
-                               _stream(stream)))
+    _check(lib().spr_embed_bwd(code, t, v, w, float(scale), _arg("ids", ids, torch.int32, (t,), dev),
+                               _arg("dy", dy, dy.dtype, (t, w), dev),
+                               _arg("dtable", dtable, torch.float32, (v, w), dev), *_ws(ws, dev),
+                               _on(dev, stream)))
 
 
 def swiglu_fwd(g, u, m, stream=None):
@@ -574,94 +594,71 @@ def experts_plan(n_experts, experts, offsets, row_token, pos, ws=None, stream=No
     """Stable sort of experts [T, k] by expert: offsets [E + 1], row_token
     [T k] and pos [T, k], all int32; ids outside [0, E) are dropped."""
     import torch
-    t, k = experts.shape
-    _typed(torch.int32, experts=experts, offsets=offsets, row_token=row_token, pos=pos)
-    _shaped((int(n_experts) + 1,), offsets=offsets)
-    _shaped((t * k,), row_token=row_token)
-    _shaped((t, k), pos=pos)
-    _check(lib().spr_experts_plan(n_experts, k, t, _ptr(experts), _ptr(offsets), _ptr(row_token), _ptr(pos), _ptr(ws),
-                                  _nbytes(ws), _stream(stream)))
+    (t, k), i32, dev = experts.shape, torch.int32, experts.get_device()
+    _check(lib().spr_experts_plan(n_experts, k, t, _arg("experts", experts, i32, (t, k), dev),
+                                  _arg("offsets", offsets, i32, (n_experts + 1,), dev),
+                                  _arg("row_token", row_token, i32, (t * k,), dev), _arg("pos", pos, i32, (t, k), dev),
+                                  *_ws(ws, dev), _on(dev, stream)))
 
 
 def experts_fwd(offsets, x, w, y, w2=None, y2=None, row_token=None, stream=None):
     """y[r] = x[row_token[r]] w[e] (x[r] without row_token) for the rows r of
     every expert e, w [E, in, out]; w2, y2: a second product of the same rows."""
     import torch
-    e, i, o = w.shape
-    rows = y.shape[0]
-    _typed(torch.bfloat16, x=x, w=w, w2=w2, y=y, y2=y2)
-    _typed(torch.int32, offsets=offsets, row_token=row_token)
-    _shaped((e + 1,), offsets=offsets)
-    _shaped((rows,), row_token=row_token)
-    _shaped((x.shape[0], i), x=x)
-    _shaped((e, i, o), w2=w2)
-    _shaped((rows, o), y=y, y2=y2)
-    _check(lib().spr_experts_fwd(e, rows, i, o, _ptr(offsets), _ptr(x), x.shape[0], _ptr(row_token), _ptr(w), _ptr(y),
-                                 _ptr(w2), _ptr(y2), _stream(stream)))
+    (e, i, o), rows, n, dev, bf, i32 = w.shape, y.shape[0], x.shape[0], w.get_device(), torch.bfloat16, torch.int32
+    _check(lib().spr_experts_fwd(e, rows, i, o, _arg("offsets", offsets, i32, (e + 1,), dev),
+                                 _arg("x", x, bf, (n, i), dev), n, _arg("row_token", row_token, i32, (rows,), dev),
+                                 _arg("w", w, bf, (e, i, o), dev), _arg("y", y, bf, (rows, o), dev),
+                                 _arg("w2", w2, bf, (e, i, o), dev), _arg("y2", y2, bf, (rows, o), dev),
+                                 _on(dev, stream)))
 
 
 def experts_bwd_x(offsets, dy, w, dx, dy2=None, w2=None, stream=None):
     """dx[r] = dy[r] w[e]^T (+ dy2[r] w2[e]^T) for the rows r of every expert."""
     import torch
-    e, i, o = w.shape
-    rows = dy.shape[0]
-    _typed(torch.bfloat16, dy=dy, w=w, dx=dx, dy2=dy2, w2=w2)
-    _typed(torch.int32, offsets=offsets)
-    _shaped((e + 1,), offsets=offsets)
-    _shaped((rows, o), dy=dy, dy2=dy2)
-    _shaped((e, i, o), w2=w2)
-    _shaped((rows, i), dx=dx)
-    _check(lib().spr_experts_bwd_x(e, rows, i, o, _ptr(offsets), _ptr(dy), _ptr(w), _ptr(dy2), _ptr(w2), _ptr(dx),
-                                   _stream(stream)))
+    (e, i, o), rows, dev, bf = w.shape, dy.shape[0], w.get_device(), torch.bfloat16
+    _check(lib().spr_experts_bwd_x(e, rows, i, o, _arg("offsets", offsets, torch.int32, (e + 1,), dev),
+                                   _arg("dy", dy, bf, (rows, o), dev), _arg("w", w, bf, (e, i, o), dev),
+                                   _arg("dy2", dy2, bf, (rows, o), dev), _arg("w2", w2, bf, (e, i, o), dev),
+                                   _arg("dx", dx, bf, (rows, i), dev), _on(dev, stream)))
 
 
 def experts_bwd_w(offsets, x, dy, dw, dy2=None, dw2=None, row_token=None, overwrite=False, stream=None):
     """dw[e] += the sum over e's rows of x[row_token[r]]^T dy[r], fp32 (written
     where ``overwrite``); dy2, dw2: a second pair of the same rows."""
     import torch
-    e, i, o = dw.shape
-    rows = dy.shape[0]
-    _typed(torch.bfloat16, x=x, dy=dy, dy2=dy2)
-    _typed(torch.float32, dw=dw, dw2=dw2)
-    _typed(torch.int32, offsets=offsets, row_token=row_token)
-    _shaped((e + 1,), offsets=offsets)
-    _shaped((rows,), row_token=row_token)
-    _shaped((x.shape[0], i), x=x)
-    _shaped((rows, o), dy=dy, dy2=dy2)
-    _shaped((e, i, o), dw2=dw2)
-    _check(lib().spr_experts_bwd_w(e, rows, i, o, _ptr(offsets), _ptr(x), x.shape[0], _ptr(row_token), _ptr(dy),
-                                   _ptr(dw), _ptr(dy2), _ptr(dw2), 1 if overwrite else 0, _stream(stream)))
+    (e, i, o), rows, n, dev, bf, i32 = dw.shape, dy.shape[0], x.shape[0], dw.get_device(), torch.bfloat16, torch.int32
+    _check(lib().spr_experts_bwd_w(e, rows, i, o, _arg("offsets", offsets, i32, (e + 1,), dev),
+                                   _arg("x", x, bf, (n, i), dev), n, _arg("row_token", row_token, i32, (rows,), dev),
+                                   _arg("dy", dy, bf, (rows, o), dev), _arg("dw", dw, torch.float32, (e, i, o), dev),
+                                   _arg("dy2", dy2, bf, (rows, o), dev),
+                                   _arg("dw2", dw2, torch.float32, (e, i, o), dev), 1 if overwrite else 0,
+                                   _on(dev, stream)))
 
 
 def experts_combine_fwd(y, pos, weights, out, add=None, stream=None):
     """out[t] = add[t] + the sum over j of weights[t, j] y[pos[t, j]]; weights
     None: ones.  A pos outside y's rows is skipped."""
     import torch
-    t, k = pos.shape
-    rows, width = y.shape
-    _typed(torch.bfloat16, y=y, out=out, add=add)
-    _typed(torch.int32, pos=pos)
-    _typed(torch.float32, weights=weights)
-    _shaped((t, k), weights=weights)
-    _shaped((t, width), out=out, add=add)
-    _check(lib().spr_experts_combine_fwd(t, k, rows, width, _ptr(y), _ptr(pos), _ptr(weights), _ptr(add), _ptr(out),
-                                         _stream(stream)))
+    (t, k), (rows, width), dev, bf = pos.shape, y.shape, y.get_device(), torch.bfloat16
+    _check(lib().spr_experts_combine_fwd(t, k, rows, width, _arg("y", y, bf, (rows, width), dev),
+                                         _arg("pos", pos, torch.int32, (t, k), dev),
+                                         _arg("weights", weights, torch.float32, (t, k), dev),
+                                         _arg("add", add, bf, (t, width), dev), _arg("out", out, bf, (t, width), dev),
+                                         _on(dev, stream)))
 
 
 def experts_combine_bwd(dout, y, pos, weights, dy, dweights, stream=None):
     """dy[pos[t, j]] = weights[t, j] dout[t], dweights[t, j] = <y[pos[t, j]],
     dout[t]>; y and dweights may both be None, weights None means ones."""
     import torch
-    t, k = pos.shape
-    rows, width = dy.shape
-    _typed(torch.bfloat16, dout=dout, y=y, dy=dy)
-    _typed(torch.int32, pos=pos)
-    _typed(torch.float32, weights=weights, dweights=dweights)
-    _shaped((t, k), weights=weights, dweights=dweights)
-    _shaped((t, width), dout=dout)
-    _shaped((rows, width), y=y)
-    _check(lib().spr_experts_combine_bwd(t, k, rows, width, _ptr(dout), _ptr(y), _ptr(pos), _ptr(weights), _ptr(dy),
-                                         _ptr(dweights), _stream(stream)))
+    (t, k), (rows, width), dev, bf, f32 = pos.shape, dy.shape, dy.get_device(), torch.bfloat16, torch.float32
+    _check(lib().spr_experts_combine_bwd(t, k, rows, width, _arg("dout", dout, bf, (t, width), dev),
+                                         _arg("y", y, bf, (rows, width), dev),
+                                         _arg("pos", pos, torch.int32, (t, k), dev),
+                                         _arg("weights", weights, f32, (t, k), dev),
+                                         _arg("dy", dy, bf, (rows, width), dev),
+                                         _arg("dweights", dweights, f32, (t, k), dev), _on(dev, stream)))
 
 
 def moe_stats_bytes(n_experts: int) -> int:

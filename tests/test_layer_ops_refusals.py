@@ -141,27 +141,40 @@ class _Cuda:
     is_cuda = True
 
     def __init__(self, shape, strides, dt=torch.bfloat16, index=0):
-        self.shape, self._s, self.dtype = shape, strides, dt
-        self.device = type("D", (), {"index": index, "__str__": lambda s: f"cuda:{index}"})()
+        self.shape, self._s, self.dtype, self.index = shape, strides, dt, index
 
-    def stride(self, i):
-        return self._s[i]
+    def stride(self):
+        return self._s
+
+    def get_device(self):
+        return self.index
+
+    def is_contiguous(self):
+        return True
 
     def data_ptr(self):
         return _at(1)
 
 
+def _rows(shape, strides):
+    return B._rows_arg("q", _Cuda(shape, strides), torch.bfloat16, shape, 0)
+
+
 def test_binding_strides_and_device(monkeypatch):
-    assert B._token_rows("q", _Cuda((5, 4, 64), (512, 64, 1))) == (_at(1), 512)
-    assert B._token_rows("q", _Cuda((1, 4, 64), (3, 64, 1))) == (_at(1), 256)
-    assert B._token_rows("q", _Cuda((5, 1, 64), (64, 7, 1))) == (_at(1), 64)
+    assert _rows((5, 4, 64), (512, 64, 1)) == (_at(1), 512)
+    assert _rows((1, 4, 64), (3, 64, 1)) == (_at(1), 256)
+    assert _rows((5, 1, 64), (64, 7, 1)) == (_at(1), 64)
     with pytest.raises(ValueError, match="not contiguous"):
-        B._token_rows("q", _Cuda((5, 4, 64), (512, 128, 1)))
+        _rows((5, 4, 64), (512, 128, 1))
     with pytest.raises(ValueError, match="not contiguous"):
-        B._token_rows("q", _Cuda((5, 4, 64), (512, 1, 4)))
+        _rows((5, 4, 64), (512, 1, 4))
     with pytest.raises(ValueError, match="tokens overlap"):
-        B._token_rows("q", _Cuda((5, 4, 64), (0, 64, 1)))
+        _rows((5, 4, 64), (0, 64, 1))
+    bf = torch.bfloat16
+    assert B._arg("q", _Cuda((2,), (1,)), bf, (2,), 0) == _at(1)
+    with pytest.raises(ValueError, match="q is on cuda:1, not on the call's device cuda:0"):
+        B._arg("q", _Cuda((2,), (1,), index=1), bf, (2,), 0)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    B._typed(torch.bfloat16, q=_Cuda((1, 1, 2), (2, 2, 1)))
-    with pytest.raises(ValueError, match="q is on cuda:1, not on the current device cuda:0"):
-        B._typed(torch.bfloat16, q=_Cuda((1, 1, 2), (2, 2, 1), index=1))
+    with pytest.raises(ValueError, match="the tensors are on cuda:1, not on the current device cuda:0"):
+        B._on(1, 5)
+    assert B._on(0, 5) == 5
