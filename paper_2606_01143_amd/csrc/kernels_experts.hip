@@ -17,6 +17,7 @@
 // (both operands: a zero times another row's infinity would be a NaN); C rows
 // and columns past the end repeat a valid address and are not stored.  A wave
 // whose rows are all past the end skips its products.
+#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -76,20 +77,22 @@ struct Natural {
   }
 };
 
-// Transposed operand: STEP contraction rows of COLS columns, in panels of 128.
+// Transposed operand: STEP contraction rows of COLS columns, in panels of 128
+// (or one of 64).
 template <int COLS, int STEP, int WAVES>
 struct Transposed {
-  static constexpr int PER = STEP / 4;  // loads of a panel, four rows each
-  static constexpr int N = COLS / 128 * PER, I = (N + WAVES - 1) / WAVES;
+  static constexpr int PW = COLS < 128 ? COLS : 128, CH = PW / 8, RPL = 64 / CH;  // chunks of a row, rows of a load
+  static constexpr int PER = STEP / RPL;  // loads of a panel
+  static constexpr int N = COLS / PW * PER, I = (N + WAVES - 1) / WAVES;
   const char* p[I];  // column of load i in row 0 of `base`
   int row[I], w;
   __device__ __forceinline__ void init(int wave, int lane, const bf16* base, int ncols) {
     w = wave;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-      const int q = (w + WAVES * i) % N;  // panel q / PER, rows 4 (q % PER) ..
-      row[i] = 4 * (q % PER) + (lane >> 4);
-      const int c = 128 * (q / PER) + 8 * ((lane & 15) ^ swz<128>(row[i]));
+      const int q = (w + WAVES * i) % N;  // panel q / PER, rows RPL (q % PER) ..
+      row[i] = RPL * (q % PER) + lane / CH;
+      const int c = PW * (q / PER) + 8 * (lane % CH ^ swz<PW>(row[i]));
       p[i] = (const char*)(base + (c < ncols ? c : 0));
     }
   }
@@ -113,8 +116,8 @@ struct Transposed {
   // element offset of 32-column block b's operand, contraction rows 8 h + 4 hi ..
   static __device__ __forceinline__ int frag(int lane, int b, int hi) {
     const int h = lane >> 5, i16 = lane & 15;
-    return (b >> 2) * STEP * 128 +
-           toff<128>(8 * h + 4 * hi + (i16 >> 2), 32 * (b & 3) + (lane & 16) + 4 * (i16 & 3));
+    return 32 * b / PW * STEP * PW +
+           toff<PW>(8 * h + 4 * hi + (i16 >> 2), 32 * b % PW + (lane & 16) + 4 * (i16 & 3));
   }
 };
 
@@ -431,13 +434,13 @@ __global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) v
       if constexpr (j != 1 && j <= NI) {
         constexpr int n = j == 0 ? 0 : j - 1;
         if constexpr (B_TR)
-          fb[v & 1][n] = tr_pair((const bf16*)(bptr[0][n] + tb + v * 4096), (const bf16*)(bptr[1][n] + tb + v * 4096));
+          fb[v & 1][n] = tr_pair((const bf16*)(bptr[0][n] + tb + v * 32 * TrB::PW), (const bf16*)(bptr[1][n] + tb + v * 32 * TrB::PW));
         else
           fb[v & 1][n] = *(const bf16x8*)(bptr[v][0] + tb + n * 64 * STEP);
       } else {
         constexpr int m = j == 1 ? 0 : j - NI;
         if constexpr (A_TR)
-          fa[v & 1][m] = tr_pair((const bf16*)(aptr[0][m] + ta + v * 4096), (const bf16*)(aptr[1][m] + ta + v * 4096));
+          fa[v & 1][m] = tr_pair((const bf16*)(aptr[0][m] + ta + v * 32 * TrA::PW), (const bf16*)(aptr[1][m] + ta + v * 32 * TrA::PW));
         else
           fa[v & 1][m] = *(const bf16x8*)(aptr[v][0] + ta + m * MW * 64 * STEP);
       }
@@ -580,26 +583,77 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
   grid = (grid + kXcds - 1) / kXcds * kXcds;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
   if (grid == 0) return hipSuccess;
-  hipLaunchKernelGGL((experts_kernel<MODE, BM, BN, MW, NW, STEP, RING, TOKENS>), dim3((unsigned)grid), dim3(64 * MW * NW), 0, st, a);
+  hipLaunchKernelGGL((experts_kernel<MODE, BM, BN, MW, NW, STEP, RING, TOKENS>), dim3((unsigned)grid), dim3(64 * MW * NW),
+                     0, st, a);
   return hipGetLastError();
+}
+
+// Which tiles.  A launch of 256 x 256 tiles runs one workgroup a CU, one of 128 x
+// 128 tiles two; the latter's CU does 0.68 of the work in a tile's time (dense
+// 1010 against 1205 TFLOP/s, and more rows and weights read).  Rounds are
+// counted from the rows' average, half a tile of padding per expert that has
+// rows; half a round is added for the last one where there are several.
+// Measured 256 / 128, us: 128 experts of 2048 x 768 top-8, forward, tokens 1024
+// 195 / 171, 2045 207 / 213, 4096 269 / 306, 8192 432 / 530; eight of 4096 x
+// 1536 top-2, 300 tokens, forward 91 / 62, row gradients 74 / 60; 1000 tokens 97
+// / 85 and 86 / 118.
+bool small_tiles(const ExpertArgs& a, int cols_of_c, int parts) {
+  const long some = std::min(a.E, a.rows);
+  auto cost = [&](long tile, long slots) {
+    const long high = std::max(some, a.rows / tile + some / 2);
+    const double rounds = (double)(high * ((cols_of_c + tile - 1) / tile) * parts) / (double)slots;
+    return rounds <= 1. ? 1. : rounds + 0.5;
+  };
+  return 0.68 * cost(128, 512) < cost(256, 256);
+}
+// Few rows an expert: the weights are all there is to read, and tiles of 32 rows
+// and 64 columns, three workgroups of two waves a CU, put more of their loads in
+// flight.  Up to four rows on average, or up to 16 where 128 x 128 tiles leave
+// CUs idle.  Measured 128 x 128 / 32 x 64, us: 128 experts of 2048 x 768 top-8,
+// forward, tokens 1 22 / 11.5, 4 38 / 36, 64 125 / 118, 256 140 / 151; eight of
+// 4096 x 1536 top-2, 1 token 38 / 16, 32 tokens 60 / 50; 60 of 1024 x 512 top-4,
+// 100 tokens 23.0 / 24.8.
+bool few_rows(const ExpertArgs& a, int cols_of_c, int parts) {
+  if ((long)a.rows <= 4L * a.E) return true;
+  return (long)a.rows <= 16L * a.E && (long)std::min(a.E, a.rows) * ((cols_of_c + 127) / 128) * parts <= 256;
+}
+
+template <int MODE>
+hipError_t launch_rows_of(const ExpertArgs& a, int cols_of_c, int parts, hipStream_t st) {
+  if (few_rows(a, cols_of_c, parts)) return launch_tiles<MODE, 32, 64, 1, 2, 64, 4>(a, st);
+  if (small_tiles(a, cols_of_c, parts)) return launch_tiles<MODE, 128, 128, 2, 2, 64, 2>(a, st);
+  return launch_tiles<MODE, 256, 256, 2, 4, 64, 2>(a, st);
+}
+
+template <bool TOKENS>
+hipError_t launch_bwd_w(const ExpertArgs& a, hipStream_t st) {
+  // An expert's tiles of C do not depend on its rows.  Half the chip or less in
+  // 256 x 256 tiles, or little more than the writes to do: 128 x 128 ones.
+  // Measured 256 / 128, us: four experts of 1024 x 1024, 8192 rows each 242 / 203;
+  // 60 of 1024 x 512, 67 rows each 58 / 50, 533 rows each 116 / 115; 64 of 2560 x
+  // 1280, 384 rows each 582 / 643.
+  const long tiles = (long)a.E * (a.b2 != nullptr ? 2 : 1) * ((a.in_width + 255) / 256) * ((a.out_width + 255) / 256);
+  if (tiles <= 128 || a.rows / a.E < 100) return launch_tiles<kBwdW, 128, 128, 2, 2, 32, 3, TOKENS>(a, st);
+  // gathered rows: longer steps, which fetch their tokens half as often
+  if constexpr (TOKENS)
+    return launch_tiles<kBwdW, 256, 256, 2, 4, 64, 2, true>(a, st);
+  else
+    return launch_tiles<kBwdW, 256, 256, 2, 4, 32, 3, false>(a, st);
 }
 
 }  // namespace
 
-constexpr int kTallRows = 128;
-
 hipError_t launch_experts_fwd(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_fwd", st);
-  return a.rows / a.E >= kTallRows ? launch_tiles<kFwd, 256, 256, 2, 4, 64, 2>(a, st) : launch_tiles<kFwd, 128, 128, 2, 2, 64, 2>(a, st);
+  return launch_rows_of<kFwd>(a, a.out_width, a.b2 != nullptr ? 2 : 1, st);
 }
 hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_x", st);
-  return a.rows / a.E >= kTallRows ? launch_tiles<kBwdX, 256, 256, 2, 4, 64, 2>(a, st) : launch_tiles<kBwdX, 128, 128, 2, 2, 64, 2>(a, st);
+  return launch_rows_of<kBwdX>(a, a.in_width, 1, st);
 }
 hipError_t launch_experts_bwd_w(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_w", st);
-  return a.row_token != nullptr ? launch_tiles<kBwdW, 256, 256, 2, 4, 64, 2, true>(a, st)
-                                : launch_tiles<kBwdW, 256, 256, 2, 4, 32, 3>(a, st);
+  return a.row_token != nullptr ? launch_bwd_w<true>(a, st) : launch_bwd_w<false>(a, st);
 }
 
 }  // namespace spr
