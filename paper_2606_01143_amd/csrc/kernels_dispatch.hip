@@ -105,7 +105,7 @@ hipError_t launch_experts_plan(int E, int k, long slots, const int* experts, int
                                void* ws, hipStream_t st) {
   const int nb = sort_ranges(slots);
   const SortPass p = {experts, slots, sort_range_items(slots, nb), E, 0, sort_bits(E), E + 1, nb, (int*)ws};
-  if (nb > 1) {
+  if (sort_counts(slots)) {
     ProfileScope ps("sort_count", st);
     hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, p);
   }

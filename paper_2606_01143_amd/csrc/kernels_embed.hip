@@ -75,15 +75,17 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortPass p, co
   });
 }
 
-// Sums of runs (the sorted tokens of one id).  A wave takes kSpan consecutive
-// sorted tokens and 512 columns (eight a lane), so that a frequent id's run is
-// shared by many waves.  A run that lies inside the span is added to its table
-// row at once; the part of one that began before it goes to head[span], the part
-// of one that begins here and goes on to tail[span], and embed_join adds those up
-// in order.  Per element that is the order of the tokens within a span, then of
-// the spans.  HBM bound: a row of dy is read once, a row of the table read and
-// written once, a part (at most two a span) written and read once.
-constexpr int kSpan = 32, kAhead = 4;
+// Sums of runs (the sorted tokens of one id).  A wave takes `len` consecutive
+// sorted tokens, a span, and 512 columns (eight a lane), so that a frequent id's
+// run is shared by many waves.  A run that lies inside the span is added to its
+// table row at once; the part of one that began before it goes to head[span], the
+// part of one that begins here and goes on to tail[span], and embed_join adds
+// those up in order.  Per element that is the order of the tokens within a span,
+// then of the spans.  HBM bound: a row of dy is read once, a row of the table read
+// and written once, a part (at most two a span) written and read once.
+// 28672 tokens x 4096 of log-uniform ids: 124 us (4.7 TB/s; one thread a run and
+// chunk 1.9 ms).
+constexpr int kAhead = 4;
 
 template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(const int* __restrict__ keys,
@@ -91,26 +93,21 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(const int* __
                                                                    const T* __restrict__ dy, float* dtable,
                                                                    float* __restrict__ head, float* __restrict__ tail,
                                                                    int tokens, int vocab, int chunks, int slabs,
-                                                                   float scale) {
+                                                                   int len, float scale) {
   const long wave = (long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long span = wave / slabs;
   const int lane = threadIdx.x & 63, chunk = (int)(wave % slabs) * 64 + lane;
-  const long p0 = span * kSpan;
+  const long p0 = span * len;
   if (p0 >= tokens) return;
-  const int n = (int)min((long)kSpan, tokens - p0);
-  // lane q holds the span's q-th key and token, lane kSpan the key behind it, and
-  // the one after that the key before it
+  const int n = (int)min((long)len, tokens - p0);
+  // lane q holds the span's q-th key and token
   int key = vocab, token = 0;
   if (lane < n) {
     key = keys[p0 + lane];
     token = order[p0 + lane];
-  } else if (lane == kSpan && p0 + kSpan < tokens) {
-    key = keys[p0 + kSpan];
-  } else if (lane == kSpan + 1 && p0 > 0) {
-    key = keys[p0 - 1];
   }
+  const int behind = p0 + len < tokens ? keys[p0 + len] : vocab, before = p0 > 0 ? keys[p0 - 1] : vocab;
   auto key_at = [&](int q) { return __builtin_amdgcn_readlane(key, q); };
-  const int behind = n == kSpan ? key_at(kSpan) : vocab, before = p0 > 0 ? key_at(kSpan + 1) : vocab;
   const bool in = chunk < chunks;
   float sum[8] = {};
   float v[kAhead][8];
@@ -156,61 +153,84 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_runs_kernel(const int* __
 }
 
 // The runs that cross spans: the wave of the span where one begins adds its
-// tail and the heads of the spans up to its end, eight at a time.
+// tail and the heads of the spans up to its end, eight at a time.  A chain of
+// dependent loads: the first head and the table's row are read while the run's
+// end is looked for (eight heads ahead would read more than most runs have: 25 us
+// instead of 12 at 28672 tokens x 4096).
 __global__ __launch_bounds__(kEmbedThreads) void embed_join_kernel(const int* __restrict__ keys, float* dtable,
                                                                    const float* __restrict__ head,
                                                                    const float* __restrict__ tail, int tokens,
-                                                                   int vocab, int chunks, int slabs, float scale) {
+                                                                   int vocab, int chunks, int slabs, int len,
+                                                                   float scale) {
   const long wave = (long)blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long span = wave / slabs, p0 = span * kSpan;
+  const long span = wave / slabs, p0 = span * len;
   const int lane = threadIdx.x & 63, chunk = (int)(wave % slabs) * 64 + lane;
-  if (p0 + kSpan >= tokens) return;
-  const int k = keys[p0 + kSpan - 1];
+  if (p0 + len >= tokens) return;
+  const int before = keys[p0 > 0 ? p0 - 1 : 0], at = keys[p0], k = keys[p0 + len - 1], next = keys[p0 + len];
   // a run begins here and goes on
-  if (k >= vocab || keys[p0 + kSpan] != k || (p0 > 0 && keys[p0] == k && keys[p0 - 1] == k)) return;
-  // its last span: the first one behind this whose last key is another, found
-  // 64 spans at a time
-  const long spans = (tokens + kSpan - 1) / kSpan;
+  if ((k >= vocab) | (next != k) | ((p0 > 0) & (at == k) & (before == k))) return;
+  const long spans = ((long)tokens + len - 1) / len;
+  const bool in = chunk < chunks;
+  float* dst = dtable + ((long)k * chunks + chunk) * 8;
+  float sum[8] = {}, old[8] = {}, one[8] = {};
+  if (in) {
+    Vec8<float>::load(tail + (span * chunks + chunk) * 8, sum);
+    Vec8<float>::load(head + ((span + 1) * chunks + chunk) * 8, one);
+    Vec8<float>::load(dst, old);
+  }
+  // the run's last span: the first one behind this that does not hold it whole
+  // and go on, found 64 spans at a time
   long end = span;
   for (long s = span + 1;; s += 64) {
     const long mine = s + lane;
-    const bool on = mine + 1 < spans && keys[mine * kSpan + kSpan - 1] == k && keys[mine * kSpan + kSpan] == k;
+    const bool on = mine + 1 < spans && keys[mine * len + len - 1] == k && keys[mine * len + len] == k;
     const unsigned long long off = __ballot(!on);
     if (off != 0) {
       end = s + __builtin_ctzll(off);
       break;
     }
   }
-  if (chunk >= chunks) return;
-  float sum[8];
-  Vec8<float>::load(tail + (span * chunks + chunk) * 8, sum);
-#pragma unroll 8
-  for (long s = span + 1; s <= end; ++s) {
-    float v[8];
-    Vec8<float>::load(head + (s * chunks + chunk) * 8, v);
+  if (!in) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += v[j];
+  for (int j = 0; j < 8; ++j) sum[j] += one[j];
+  for (long s = span + 2; s <= end; s += 8) {
+    float v[8][8] = {};
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (s + q <= end) Vec8<float>::load(head + ((s + q) * chunks + chunk) * 8, v[q]);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[q][j];
   }
-  float* dst = dtable + ((long)k * chunks + chunk) * 8;
-  float old[8];
-  Vec8<float>::load(dst, old);
 #pragma unroll
   for (int j = 0; j < 8; ++j) old[j] = fmaf(scale, sum[j], old[j]);
   Vec8<float>::store(dst, old);
 }
 
 namespace {
+// Tokens of a span: a power of two that leaves about 4096 waves (four a SIMD),
+// from 8 to the 64 that a wave holds keys of.  Short spans cross more runs, whose
+// parts are written and read again; long ones leave CUs idle.  Whole call, us,
+// with 2048 / 4096 / 8192 waves as the aim, width 4096: 28672 tokens 179 / 163 /
+// 178, 8192 tokens 87 / 73 / 75, 28672 tokens of 500 ids 91 / 83 / 94.
+int embed_span(long n, long slabs) {
+  int len = 8;
+  while (len < 64 && 2 * len * 4096L <= n * slabs) len *= 2;
+  return len;
+}
 // workspace: two buffers of keys and tokens, the histograms, then the parts of
 // runs that cross spans (none where one span holds all tokens)
 struct EmbedWs {
   size_t item, hist, head, tail, total;
 };
 EmbedWs embed_ws(long n, long width) {
+  const int len = embed_span(n, (width / 8 + 63) / 64);
   EmbedWs w;
   w.item = ((size_t)n * 4 + 255) / 256 * 256;
   w.hist = 4 * w.item;
   w.head = w.hist + (sort_hist_bytes(n, 1 << kSortRadixBits) + 255) / 256 * 256;
-  const size_t part = n > kSpan ? (size_t)((n + kSpan - 1) / kSpan) * width * 4 : 0;
+  const size_t part = n > len ? (size_t)((n + len - 1) / len) * width * 4 : 0;
   w.tail = w.head + part;
   w.total = w.tail + part;
   return w;
@@ -251,7 +271,7 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
   for (int shift = 0, left = sort_bits(vocab); left > 0; left -= kSortRadixBits, shift += kSortRadixBits) {
     const int bits = left < kSortRadixBits ? left : kSortRadixBits;
     const SortPass p = {k_in, n, per, vocab, shift, bits, 1 << bits, nb, hist};
-    if (nb > 1) {
+    if (sort_counts(n)) {
       ProfileScope ps("sort_count", st);
       hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, p);
     }
@@ -261,24 +281,24 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
     t_in = order[out];
     out ^= 1;
   }
-  const int chunks = width / 8, slabs = (chunks + 63) / 64;
+  const int chunks = width / 8, slabs = (chunks + 63) / 64, len = embed_span(n, slabs);
   float* head = (float*)(base + w.head);
   float* tail = (float*)(base + w.tail);
-  const long waves = (n + kSpan - 1) / kSpan * slabs;
+  const long waves = (n + len - 1) / len * slabs;
   const dim3 grid((unsigned)((waves + kEmbedThreads / 64 - 1) / (kEmbedThreads / 64)));
   {
     ProfileScope ps("embed_runs", st);
     if (dtype == 1)
       hipLaunchKernelGGL(embed_runs_kernel<bf16>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const bf16*)dy,
-                         dtable, head, tail, tokens, vocab, chunks, slabs, scale);
+                         dtable, head, tail, tokens, vocab, chunks, slabs, len, scale);
     else
       hipLaunchKernelGGL(embed_runs_kernel<float>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const float*)dy,
-                         dtable, head, tail, tokens, vocab, chunks, slabs, scale);
+                         dtable, head, tail, tokens, vocab, chunks, slabs, len, scale);
   }
-  if (n > kSpan) {
+  if (n > len) {
     ProfileScope ps("embed_join", st);
     hipLaunchKernelGGL(embed_join_kernel, grid, dim3(kEmbedThreads), 0, st, k_in, dtable, head, tail, tokens, vocab,
-                       chunks, slabs, scale);
+                       chunks, slabs, len, scale);
   }
   return hipGetLastError();
 }

@@ -591,7 +591,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
 // Which tiles.  A launch of 256 x 256 tiles runs one workgroup a CU, one of 128 x
 // 128 tiles two; the latter's CU does 0.68 of the work in a tile's time (dense
 // 1010 against 1205 TFLOP/s, and more rows and weights read).  Rounds are
-// counted from the rows' average, half a tile of padding per expert that has
+// counted from the rows' average, a good half tile of padding per expert that has
 // rows; half a round is added for the last one where there are several.
 // Measured 256 / 128, us: 128 experts of 2048 x 768 top-8, forward, tokens 1024
 // 195 / 171, 2045 207 / 213, 4096 269 / 306, 8192 432 / 530; eight of 4096 x
@@ -600,7 +600,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
 bool small_tiles(const ExpertArgs& a, int cols_of_c, int parts) {
   const long some = std::min(a.E, a.rows);
   auto cost = [&](long tile, long slots) {
-    const long high = std::max(some, a.rows / tile + some / 2);
+    const long high = std::max(some, a.rows / tile + some * 11 / 20);
     const double rounds = (double)(high * ((cols_of_c + tile - 1) / tile) * parts) / (double)slots;
     return rounds <= 1. ? 1. : rounds + 0.5;
   };

@@ -1,17 +1,18 @@
 // Stable counting sort of int32 keys on the device, one digit of a pass at a
 // time: positions of the keys in (key, index) order, the same every run.
 //
-// A pass cuts the items into equal ranges, one per workgroup.  sort_count writes
-// each range's histogram; the placing kernel adds up the histograms before its
-// own (all smaller digits, and its digit in earlier ranges) and walks its range
-// 1024 items at a time: a wave's equal digits are matched with one ballot per
-// bit, their counts are summed over the sixteen waves through LDS, and the
-// running start of each digit moves on.  Few items are one range, whose
-// workgroup counts for itself.  Only integer counts are added atomically, so no
-// result depends on an order of execution.
+// A pass cuts the items into equal ranges, one per workgroup.  A range's places
+// need the counts of all items, and of those before it: sort_count writes each
+// range's histogram first, or, of up to 4096 items, every workgroup counts all
+// of them itself and the launch is saved.  (Of 28672 items too, a pass took 20
+// us instead of 12: the counting's conflicts in LDS.)  The placing kernel walks
+// its range 1024 items at a time: a wave's equal digits are matched with one
+// ballot per bit, their counts are summed over the sixteen waves through LDS,
+// and the running start of each digit moves on.  Only integer counts are added
+// atomically, so no result depends on an order of execution.
 //
-// Latency bound.  28672 keys below 128000 (two passes of nine bits): 23 us;
-// with 256 threads a workgroup 40 us.
+// Latency bound.  28672 keys below 128000, two passes of nine bits: 23 us (with
+// 256 threads a workgroup 40).
 #pragma once
 
 #include "launch.hpp"
@@ -22,23 +23,23 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSortMaxBins = 1025;   // 1024 experts and the dropped choices
 constexpr int kSortRadixBits = 9;    // a pass of a longer key
 constexpr int kSortMaxRanges = 64;
-constexpr int kSortAlone = 2048;     // items of one workgroup that counts itself
+constexpr long kSortSelfCount = 4096;  // items that every workgroup counts for itself
 
 // keys outside [0, limit) sort last, as `limit`
 __device__ __forceinline__ int sort_key(int id, int limit) { return (unsigned)id < (unsigned)limit ? id : limit; }
 
 inline int sort_ranges(long n) {
-  if (n <= kSortAlone) return 1;
   const long r = (n + kSortThreads - 1) / kSortThreads;
-  return (int)(r > kSortMaxRanges ? kSortMaxRanges : r);
+  return (int)(r < 1 ? 1 : r > kSortMaxRanges ? kSortMaxRanges : r);
 }
+inline bool sort_counts(long n) { return n > kSortSelfCount; }  // sort_count runs first
 inline long sort_range_items(long n, int nb) { return ((n + nb - 1) / nb + kSortThreads - 1) / kSortThreads * kSortThreads; }
 inline int sort_bits(long top) {  // bits of keys 0 .. top
   int b = 1;
   while (b < 31 && (top >> b) != 0) ++b;
   return b;
 }
-inline size_t sort_hist_bytes(long n, int bins) { return (size_t)sort_ranges(n) * bins * 4; }
+inline size_t sort_hist_bytes(long n, int bins) { return sort_counts(n) ? (size_t)sort_ranges(n) * bins * 4 : 0; }
 
 // One digit of the keys.
 struct SortPass {
@@ -72,8 +73,13 @@ __device__ __forceinline__ void sort_bases(SortLds& s, const SortPass& p, int* s
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, bins = p.bins;
   for (int i = t; i < bins; i += kSortThreads) s.base[i] = s.total[i] = 0;
   __syncthreads();
-  if (p.ranges == 1) {
-    for (long i = t; i < p.n; i += kSortThreads) atomicAdd(&s.total[p.digit(sort_key(p.keys[i], p.limit))], 1);
+  if (p.n <= kSortSelfCount) {
+    // base: items before this range; total: the others, and then all
+    const int n = (int)p.n, lo = (int)(blockIdx.x * p.per);
+#pragma unroll 4
+    for (int i = t; i < n; i += kSortThreads) atomicAdd((i < lo ? s.base : s.total) + p.digit(sort_key(p.keys[i], p.limit)), 1);
+    __syncthreads();
+    for (int i = t; i < bins; i += kSortThreads) s.total[i] += s.base[i];
   } else {
     // threads beyond one per bin share the ranges
     const int groups = max(1, kSortThreads / bins), block = blockIdx.x;

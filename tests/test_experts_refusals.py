@@ -31,8 +31,10 @@ COMBINE_BWD = dict(T=10, k=2, rows=20, w=64, dout=_at(1), y=_at(2), pos=_at(3), 
     (dict(E=0), "UNSUPPORTED"), (dict(E=1025), "UNSUPPORTED"), (dict(k=0), "INVALID_ARG"), (dict(k=17), "INVALID_ARG"),
     (dict(T=-1), "INVALID_ARG"), (dict(T=2147483647), "INVALID_ARG"), (dict(experts=None), "INVALID_ARG"),
     (dict(offsets=None), "INVALID_ARG"), (dict(pos=_at(4, 2)), "MISALIGNED"), (dict(pos=_at(1)), "ALIASING"),
-    (dict(row_token=_at(4, 8)), "ALIASING"), (dict(ws=None), "WORKSPACE"), (dict(wsb=4), "WORKSPACE"),
-    (dict(ws=_at(5, 4)), "MISALIGNED"), (dict(ws=_at(2)), "ALIASING")])
+    (dict(row_token=_at(4, 8)), "ALIASING"),
+    # more than 4096 choices: the plan needs its workspace
+    (dict(T=40000, ws=None), "WORKSPACE"), (dict(T=40000, wsb=4), "WORKSPACE"),
+    (dict(T=40000, ws=_at(5, 4)), "MISALIGNED"), (dict(T=40000, ws=_at(2)), "ALIASING")])
 def test_plan(kw, status):
     assert _call("spr_experts_plan", PLAN, **kw) == "SPR_ERR_" + status
     assert B.last_error()
@@ -98,8 +100,9 @@ def test_nothing_to_do_launches_nothing():
 
 
 def test_plan_workspace_size():
-    small, large = B.experts_plan_workspace_size(8, 2, 1), B.experts_plan_workspace_size(1024, 8, 1 << 20)
-    assert 0 < small < large <= 1 << 20
+    assert B.experts_plan_workspace_size(8, 2, 2048) == 0
+    mid, large = B.experts_plan_workspace_size(8, 2, 2049), B.experts_plan_workspace_size(1024, 8, 1 << 20)
+    assert 0 < mid < large <= 1 << 20
     with pytest.raises(B.SprError):
         B.experts_plan_workspace_size(8, 9, 4)
 

@@ -46,7 +46,9 @@ def _want(E, ids):
     (1, 1, 1, "any"), (1, 8, 128, "any"), (4, 8, 128, "any"), (63, 3, 5, "any"), (129, 8, 8, "any"),
     (1000, 2, 1024, "any"), (8192, 8, 128, "any"), (3001, 4, 60, "padded"), (257, 6, 64, "dropped"),
     (500, 8, 256, "one"), (70001, 1, 7, "padded"), (20000, 8, 1023, "padded"), (40, 2, 3, "twice"), (0, 4, 16, "any"),
-    (512, 8, 128, "any"), (513, 8, 128, "any"), (1024, 1, 2, "any")])
+    (512, 8, 128, "any"), (513, 8, 128, "any"), (1024, 1, 2, "any"),
+    # either side of the count in a launch of its own
+    (4096, 1, 1024, "padded"), (4097, 1, 1024, "padded"), (2049, 2, 2, "any")])
 def test_plan(gpu, T, k, E, kind):
     import torch
     _say(f"T {T} k {k} E {E} {kind}")

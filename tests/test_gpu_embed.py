@@ -54,7 +54,10 @@ CASES = [(1, 7, 8, "any", "bf16"), (5, 1, 64, "one", "f32"), (64, 100, 520, "any
          (333, 1000, 136, "frequent", "f32"), (1000, 3, 64, "any", "bf16"), (257, 513, 24, "padded", "bf16"),
          (4097, 128000, 64, "frequent", "bf16"), (1024, 511, 40, "any", "f32"), (2000, 40, 72, "one", "bf16"),
          (3000, 262144, 16, "few", "f32"), (129, 65, 4096, "padded", "f32"), (50, 9, 16, "dropped", "bf16"),
-         (20011, 50000, 8, "frequent", "f32"), (70001, 300, 8, "any", "bf16"), (2049, 2147483, 8, "any", "bf16")]
+         (20011, 50000, 8, "frequent", "f32"), (70001, 300, 8, "any", "bf16"), (2049, 2147483, 8, "any", "bf16"),
+         # either side of the count in a launch of its own, and many spans of one id
+         (4096, 700, 8, "frequent", "f32"), (65537, 700, 8, "frequent", "f32"), (33, 5, 8, "one", "bf16"),
+         (32, 5, 8, "few", "f32"), (40000, 100, 72, "padded", "bf16")]
 
 
 @pytest.mark.parametrize("T,V,width,kind,dt", CASES)
