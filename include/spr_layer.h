@@ -52,7 +52,8 @@ spr_status spr_rope_bwd(int32_t tokens, int32_t heads, int32_t head_dim, int32_t
  *   heads), so both may be views of one fused projection; any element
  *   alignment, 16 bytes (and strides of as much, d a multiple of 16) being
  *   the fast one.  gain_q, gain_k [d].  yq, yk contiguous, out; they overlap
- *   nothing.  tokens * (q_heads + kv_heads) is at most 2^31 - 1. */
+ *   nothing.  tokens * (q_heads + kv_heads), and a token's elements, are at most
+ * 2^31 - 1. */
 spr_status spr_head_norm_rope_fwd(int32_t dtype, int32_t tokens, int32_t q_heads, int32_t kv_heads,
                                   int32_t head_dim, float eps, int32_t pos0, const int32_t* positions,
                                   double theta, const void* q, int64_t q_stride, const void* k,

@@ -1516,6 +1516,7 @@ spr_status check_heads(int32_t dtype, int32_t tokens, int32_t hq, int32_t hkv, i
   if ((st = check_rope(tokens, hq, d, pos0, theta)) != SPR_OK) return st;
   if ((int64_t)tokens * ((int64_t)hq + hkv) > INT32_MAX)
     return fail(SPR_ERR_INVALID_ARG, "tokens * (q_heads + kv_heads) exceeds 2^31 - 1");
+  if (((int64_t)hq + hkv) * d > INT32_MAX) return fail(SPR_ERR_INVALID_ARG, "a token's heads exceed 2^31 - 1 elements");
   if (!(eps >= 0.f) || isinf(eps)) return fail(SPR_ERR_INVALID_ARG, "eps must be finite and >= 0");
   return SPR_OK;
 }

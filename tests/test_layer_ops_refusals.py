@@ -33,7 +33,8 @@ SIZES = [(dict(dtype=2), "UNSUPPORTED"), (dict(T=-1), "INVALID_ARG"), (dict(hq=0
          (dict(d=0), "UNSUPPORTED"), (dict(eps=-1.0), "INVALID_ARG"), (dict(eps=float("nan")), "INVALID_ARG"),
          (dict(eps=float("inf")), "INVALID_ARG"), (dict(pos0=-1), "INVALID_ARG"), (dict(theta=1.0), "INVALID_ARG"),
          (dict(theta=float("inf")), "INVALID_ARG"), (dict(qs=255), "INVALID_ARG"), (dict(ks=127), "INVALID_ARG"),
-         (dict(qs=1 << 40), "INVALID_ARG"), (dict(T=1 << 30), "INVALID_ARG"), (dict(q=None), "INVALID_ARG"),
+         (dict(qs=1 << 40), "INVALID_ARG"), (dict(T=1 << 30), "INVALID_ARG"),
+         (dict(T=1, hq=1 << 25, qs=1 << 31), "INVALID_ARG"), (dict(q=None), "INVALID_ARG"),
          (dict(gk=None), "INVALID_ARG"), (dict(q=_at(1, 1)), "MISALIGNED"), (dict(gq=_at(2, 1)), "MISALIGNED"),
          (dict(pos=_at(20, 2)), "MISALIGNED")]
 
