@@ -11,7 +11,8 @@ cache injected into attention's prefix K/V gradient.  Weight gradients
 are the prefix part once plus every suffix part (App. A.6), accumulated in
 fp32.
 
-The token-wise operations (RMSNorm, RoPE, SwiGLU) are the library's
+The token-wise operations (RMSNorm, RoPE, SwiGLU, and the per-head norm of
+queries and keys where the weights hold its gains) are the library's
 kernels, attention is the library's schedule calls, and the projections
 are BLAS GEMMs (torch.matmul on the GPU, which ROCm serves with
 hipBLASLt).  Forward and backward are written out by hand; nothing here
@@ -27,6 +28,9 @@ import torch
 from . import binding as B
 
 W_KEYS = ("wq", "wk", "wv", "wo", "wg", "wu", "wd")
+# optional gains [head_dim] of a per-head RMS norm of queries and keys before
+# the rotary embedding (both or neither)
+HEAD_GAINS = ("gq", "gk")
 
 
 class DecoderLayer:
@@ -34,7 +38,8 @@ class DecoderLayer:
         shp = inp["shape"]
         dev = torch.device(device)
         up = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(device=dev, dtype=torch.bfloat16)
-        self._setup(shp, {k: up(inp["weights"][k]) for k in W_KEYS}, dev, None)
+        gains = tuple(k for k in HEAD_GAINS if k in inp["weights"])
+        self._setup(shp, {k: up(inp["weights"][k]) for k in W_KEYS + gains}, dev, None)
         self.x_p = up(inp["x_p"])
         self.x_s = [up(x) for x in inp["x_s"]]
         self.dy_s = [up(x) for x in inp["dy_s"]]
@@ -54,9 +59,12 @@ class DecoderLayer:
     def _setup(self, shp, weights, dev, ws):
         if shp.dtype != "bf16":
             raise ValueError("the layer path runs in bf16")
+        if ("gq" in weights) != ("gk" in weights):
+            raise ValueError("the gains of queries and keys go together")
         self.shape = shp
         self.dev = dev
         self.w = weights
+        self.head_norm = "gq" in weights
         hq, hkv, d, P = shp.num_q_heads, shp.num_kv_heads, shp.head_dim, shp.prefix_len
         self.dims = B.make_dims(hq, hkv, d, P, "bf16")
         self.gk = torch.zeros(P, hkv, d, dtype=torch.float32, device=self.dev)
@@ -64,6 +72,10 @@ class DecoderLayer:
         if ws is None:
             ws = torch.empty(self.workspace_bytes(shp), dtype=torch.uint8, device=self.dev)
         self.ws = ws
+        if self.head_norm:
+            longest = P + max(shp.suffix_lens, default=0)
+            self.ws_heads = torch.empty(B.head_norm_rope_bwd_workspace_size(longest, hq, hkv, d), dtype=torch.uint8,
+                                        device=self.dev)
         self._cu = {}
         self._dense_dims = {}
 
@@ -85,8 +97,12 @@ class DecoderLayer:
         k = (c["n1"] @ w["wk"]).view(T, hkv, d)
         c["v"] = (c["n1"] @ w["wv"]).view(T, hkv, d)
         c["q"], c["k"] = e(T, hq, d), e(T, hkv, d)
-        B.rope_fwd(q, c["q"], pos0, shp.rope_theta)
-        B.rope_fwd(k, c["k"], pos0, shp.rope_theta)
+        if self.head_norm:
+            c["q0"], c["k0"] = q, k
+            B.head_norm_rope_fwd(q, k, w["gq"], w["gk"], c["q"], c["k"], pos0, shp.rope_theta, eps=shp.norm_eps)
+        else:
+            B.rope_fwd(q, c["q"], pos0, shp.rope_theta)
+            B.rope_fwd(k, c["k"], pos0, shp.rope_theta)
         c["o"], c["lse"] = e(T, hq, d), e(T, hq, dt=torch.float32)
         attend(c)
         c["h"] = x + c["o"].view(T, -1) @ w["wo"]
@@ -118,8 +134,15 @@ class DecoderLayer:
         dk_r, dv = torch.empty_like(c["k"]), torch.empty_like(c["v"])
         attend_bwd(c, do, dq_r, dk_r, dv)
         dq, dk = torch.empty_like(dq_r), torch.empty_like(dk_r)
-        B.rope_bwd(dq_r, dq, pos0, shp.rope_theta)
-        B.rope_bwd(dk_r, dk, pos0, shp.rope_theta)
+        if self.head_norm:
+            first = dw["gq"] is None
+            if first:
+                dw["gq"], dw["gk"] = (torch.empty(d, dtype=torch.float32, device=self.dev) for _ in range(2))
+            B.head_norm_rope_bwd(c["q0"], c["k0"], w["gq"], w["gk"], dq_r, dk_r, dq, dk, dw["gq"], dw["gk"], pos0,
+                                 shp.rope_theta, eps=shp.norm_eps, overwrite=first, ws=self.ws_heads)
+        else:
+            B.rope_bwd(dq_r, dq, pos0, shp.rope_theta)
+            B.rope_bwd(dk_r, dk, pos0, shp.rope_theta)
         dq2, dk2, dv2 = dq.view(T, -1), dk.view(T, -1), dv.view(T, -1)
         dn1 = dq2 @ w["wq"].t() + dk2 @ w["wk"].t() + dv2 @ w["wv"].t()
         self._add_dw(dw, "wq", c["n1"].t() @ dq2)
