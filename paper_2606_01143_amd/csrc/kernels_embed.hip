@@ -63,6 +63,94 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(const int* __r
   Vec8<T>::store(y + 8 * i, v);
 }
 
+// Up to kFewTokens tokens: no sort and one launch.  The wave of a token and 512
+// columns holds all ids, four a lane; where the token is its id's first, it adds
+// up the rows of all of the id's tokens in order, eight at a time.
+constexpr int kFewTokens = 256;
+
+template <typename T>
+__global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const int* __restrict__ ids,
+                                                                  const T* __restrict__ dy, float* dtable, int tokens,
+                                                                  int vocab, int chunks, int slabs, float scale) {
+  const int wave = blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = wave / slabs, lane = threadIdx.x & 63, chunk = wave % slabs * 64 + lane;
+  if (t >= tokens) return;
+  const int id = ids[t];
+  if ((unsigned)id >= (unsigned)vocab) return;
+  const bool in = chunk < chunks;
+  float* dst = dtable + ((long)id * chunks + chunk) * 8;
+  float old[8] = {}, sum[8] = {};
+  if (in) Vec8<float>::load(dst, old);
+  unsigned long long same[kFewTokens / 64];
+#pragma unroll
+  for (int c = 0; c < kFewTokens / 64; ++c) {
+    const int j = 64 * c + lane;
+    same[c] = __ballot(j < tokens && ids[min(j, tokens - 1)] == id);
+  }
+  // the next of the id's tokens, or -1
+  auto next = [&]() -> int {
+    int at = -1;
+#pragma unroll
+    for (int c = kFewTokens / 64 - 1; c >= 0; --c)
+      if (same[c] != 0) at = 64 * c + __builtin_ctzll(same[c]);
+#pragma unroll
+    for (int c = 0; c < kFewTokens / 64; ++c)
+      if (at >= 0 && at >> 6 == c) same[c] &= same[c] - 1;
+    return at;
+  };
+  int row = next();
+  if (row != t) return;  // an earlier token's wave does it
+  while (row >= 0) {
+    float v[8][8] = {};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (row >= 0) {
+        if (in) Vec8<T>::load(dy + ((long)row * chunks + chunk) * 8, v[q]);
+        row = next();
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[q][j];
+  }
+  if (!in) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) old[j] = fmaf(scale, sum[j], old[j]);
+  Vec8<float>::store(dst, old);
+}
+
+// Up to kRankTokens tokens: a token's place is the number of keys that sort
+// before it, counted by eight lanes (two radix passes take two launches).
+constexpr int kRankTokens = 4096, kRankLanes = 8;
+
+__global__ __launch_bounds__(kEmbedThreads) void embed_rank_kernel(const int* __restrict__ ids, int tokens, int vocab,
+                                                                   int* __restrict__ keys_out,
+                                                                   int* __restrict__ tokens_out) {
+  __shared__ unsigned keys[kRankTokens];
+  // whole rounds of 4 keys a lane; the places behind the last token sort last
+  const int round = 4 * kRankLanes, padded = (tokens + round - 1) / round * round;
+  for (int i = threadIdx.x; i < padded; i += kEmbedThreads)
+    keys[i] = i < tokens ? (unsigned)sort_key(ids[i], vocab) : 0xffffffffu;
+  __syncthreads();
+  const int mine = blockIdx.x * (kEmbedThreads / kRankLanes) + threadIdx.x / kRankLanes, part = threadIdx.x % kRankLanes;
+  if (mine >= tokens) return;
+  const unsigned key = keys[mine];
+  int before = 0;
+#pragma unroll 4
+  for (int j = 4 * part; j < padded; j += round) {
+    const uint4 k = *(const uint4*)(keys + j);
+    before += (k.x < key + (j < mine)) + (k.y < key + (j + 1 < mine)) + (k.z < key + (j + 2 < mine)) +
+              (k.w < key + (j + 3 < mine));
+  }
+#pragma unroll
+  for (int o = 1; o < kRankLanes; o <<= 1) before += __shfl_xor(before, o);
+  if (part == 0) {
+    keys_out[before] = (int)key;
+    tokens_out[before] = mine;
+  }
+}
+
 // one pass of the sort: keys and the tokens they belong to
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortPass p, const int* __restrict__ tokens,
                                                                   int* __restrict__ keys_out,
@@ -237,7 +325,9 @@ EmbedWs embed_ws(long n, long width) {
 }
 }  // namespace
 
-size_t embed_bwd_ws(long tokens, int vocab, int width) { return tokens == 0 ? 0 : embed_ws(tokens, width).total; }
+size_t embed_bwd_ws(long tokens, int vocab, int width) {
+  return tokens <= kFewTokens ? 0 : embed_ws(tokens, width).total;
+}
 
 hipError_t launch_embed_fwd(int dtype, int tokens, int vocab, int width, float scale, const int* ids,
                             const void* table, void* y, hipStream_t st) {
@@ -258,6 +348,18 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
                             float* dtable, void* ws, hipStream_t st) {
   const long n = tokens;
   if (n == 0) return hipSuccess;
+  if (n <= kFewTokens) {
+    ProfileScope ps("embed_few", st);
+    const int few_slabs = (width / 8 + 63) / 64;
+    const dim3 few_grid((unsigned)((n * few_slabs + kEmbedThreads / 64 - 1) / (kEmbedThreads / 64)));
+    if (dtype == 1)
+      hipLaunchKernelGGL(embed_few_kernel<bf16>, few_grid, dim3(kEmbedThreads), 0, st, ids, (const bf16*)dy, dtable,
+                         tokens, vocab, width / 8, few_slabs, scale);
+    else
+      hipLaunchKernelGGL(embed_few_kernel<float>, few_grid, dim3(kEmbedThreads), 0, st, ids, (const float*)dy, dtable,
+                         tokens, vocab, width / 8, few_slabs, scale);
+    return hipGetLastError();
+  }
   const EmbedWs w = embed_ws(n, width);
   char* base = (char*)ws;
   int* keys[2] = {(int*)base, (int*)(base + w.item)};
@@ -268,7 +370,15 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
   const int* k_in = ids;
   const int* t_in = nullptr;
   int out = 0;
-  for (int shift = 0, left = sort_bits(vocab); left > 0; left -= kSortRadixBits, shift += kSortRadixBits) {
+  if (n <= kRankTokens) {
+    ProfileScope ps("embed_rank", st);
+    constexpr int per_block = kEmbedThreads / kRankLanes;
+    hipLaunchKernelGGL(embed_rank_kernel, dim3((tokens + per_block - 1) / per_block), dim3(kEmbedThreads), 0, st, ids,
+                       tokens, vocab, keys[0], order[0]);
+    k_in = keys[0];
+    t_in = order[0];
+  }
+  for (int shift = 0, left = n <= kRankTokens ? 0 : sort_bits(vocab); left > 0; left -= kSortRadixBits, shift += kSortRadixBits) {
     const int bits = left < kSortRadixBits ? left : kSortRadixBits;
     const SortPass p = {k_in, n, per, vocab, shift, bits, 1 << bits, nb, hist};
     if (sort_counts(n)) {

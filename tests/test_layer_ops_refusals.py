@@ -99,7 +99,8 @@ def test_embed_refusals(kw, status):
                                        (dict(ws=_at(4, 8)), "MISALIGNED"), (dict(ws=_at(3)), "ALIASING"),
                                        (dict(ws=_at(1)), "ALIASING")])
 def test_embed_workspace(kw, status):
-    assert _embed(False, **kw) == "SPR_ERR_" + status
+    assert _embed(False, T=300, **kw) == "SPR_ERR_" + status  # up to 256 tokens need no workspace
+    assert B.embed_bwd_workspace_size(256, 100, 64) == 0 < B.embed_bwd_workspace_size(257, 100, 64)
 
 
 def _cpu(*shape, dt=torch.bfloat16):
