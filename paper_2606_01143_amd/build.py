@@ -30,25 +30,14 @@ COMMON_FLAGS = [
     # code, and AGPR results would cost a copy per element
     "-mllvm", "-amdgpu-mfma-vgpr-form",
 ]
-# The grouped products only read their results at the end, and their largest
-# tile holds 256 of them a lane beside its operands: results in AGPRs, which
-# take no vector register (in VGPRs its loop would copy 75 of them a step).
-AGPR_SOURCES = {"kernels_experts.hip"}
 
 
 def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".hip"))
 
 
-def flags_of(src: str):
-    if os.path.basename(src) not in AGPR_SOURCES:
-        return COMMON_FLAGS
-    form = COMMON_FLAGS.index("-amdgpu-mfma-vgpr-form")
-    return COMMON_FLAGS[:form - 1] + COMMON_FLAGS[form + 1:]
-
-
 def _compile(src: str, obj: str) -> str:
-    cmd = [HIPCC, *flags_of(src), "-c", src, "-o", obj]
+    cmd = [HIPCC, *COMMON_FLAGS, "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {os.path.basename(src)}:\n{r.stderr}")

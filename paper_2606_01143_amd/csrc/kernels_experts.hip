@@ -21,7 +21,7 @@
 // bytes into LDS and took 582 us for the first figure) 128 experts of 2048 x 768,
 // 8192 tokens of top-8: gate and up 430 us (960 TFLOP/s; a plain matrix product
 // of the same operations reaches 1182 in the library), row gradients of both 474
-// us (870), weight gradients of both 660 us (625 TFLOP/s, 2.4 TB/s of fp32
+// us (870), weight gradients of both 670 us (615 TFLOP/s, 2.4 TB/s of fp32
 // gradients written).  Eight experts of 4096 x 1536: 1138, 1090 and 1205 TFLOP/s.
 //
 // Ragged ends: contraction indices past the end are read from a line of zeros
@@ -198,9 +198,9 @@ struct GroupTile {
 
 // Tile t of the launch: experts in order, each expert's ceil(len / BM) rows of
 // tiles in bands of kBand rows, a band column by column (`cols` columns).  The
-// 64 workgroups that an XCD runs at once then share kBand tiles of rows and
-// most columns of the weights.  A wave adds
-// up the experts' tile rows 64 ranges at a time and finds the one that holds t.
+// 32 large tiles that an XCD runs at once then share kBand tiles of rows and
+// eight columns of the weights.  A wave adds up the experts' tile rows, a range
+// of experts a lane, and finds the range that holds t.
 // The workgroups of one XCD (blockIdx modulo 8) take consecutive tiles, which
 // share an expert's weights and rows in its L2.
 template <int BM>
@@ -253,7 +253,7 @@ __host__ __device__ __forceinline__ int bwd_w_share(int tiles) { return (tiles +
 
 // TOKENS: the contraction rows of bwd_w are gathered
 template <int MODE, int BM, int BN, int MW, int NW, int STEP, int RING, bool TOKENS>
-__global__ __launch_bounds__(64 * MW * NW, BM / MW * (BN / NW) > 8192 ? 1 : 2) void experts_kernel(ExpertArgs a) {
+__global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) {
   constexpr int WAVES = MW * NW, MI = BM / 32 / MW, NI = BN / 32 / NW;
   constexpr bool A_TR = MODE == kBwdW, B_TR = MODE != kBwdX;
   constexpr int A_ELEMS = BM * STEP, B_ELEMS = BN * STEP, SLICES = STEP / 16;
