@@ -190,6 +190,13 @@ __device__ __forceinline__ void wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(N) : "memory");
 }
 
+// Pairs of operands: with a second result, or in bwd_x a second product to add.
+// (Without rows bwd_w's dy2 may be NULL where there is a dw2 to clear.)
+template <int MODE>
+__host__ __device__ __forceinline__ int pairs(const ExpertArgs& a) {
+  return (MODE == kBwdX ? a.b2 : a.c2) != nullptr ? 2 : 1;
+}
+
 // A workgroup's tile: expert, its rows, first row and column of C.
 struct GroupTile {
   int e, lo, len, m0, n0, part;
@@ -269,7 +276,7 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
   const int r = lane & 31, h = lane >> 5;
   // columns of C, and of tiles: C is [rows, out_width], [rows, in_width] or [in_width, out_width]
   const int ncols = MODE == kBwdX ? a.in_width : a.out_width;
-  const int tiles_n = (ncols + BN - 1) / BN, parts = a.b2 != nullptr ? 2 : 1;
+  const int tiles_n = (ncols + BN - 1) / BN, parts = pairs<MODE>(a);
 
   GroupTile g;
   if constexpr (MODE == kBwdW) {
@@ -581,7 +588,7 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
 
 template <int MODE, int BM, int BN, int MW, int NW, int STEP, int RING, bool TOKENS = false>
 hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
-  const int ncols = MODE == kBwdX ? a.in_width : a.out_width, parts = a.b2 != nullptr ? 2 : 1;
+  const int ncols = MODE == kBwdX ? a.in_width : a.out_width, parts = pairs<MODE>(a);
   const long tiles_n = (ncols + BN - 1) / BN;
   long grid;
   if (MODE == kBwdW) {
@@ -643,7 +650,7 @@ hipError_t launch_bwd_w(const ExpertArgs& a, hipStream_t st) {
   // Measured 256 / 128, us: four experts of 1024 x 1024, 8192 rows each 242 / 203;
   // 60 of 1024 x 512, 67 rows each 58 / 50, 533 rows each 116 / 115; 64 of 2560 x
   // 1280, 384 rows each 582 / 643.
-  const long tiles = (long)a.E * (a.b2 != nullptr ? 2 : 1) * ((a.in_width + 255) / 256) * ((a.out_width + 255) / 256);
+  const long tiles = (long)a.E * pairs<kBwdW>(a) * ((a.in_width + 255) / 256) * ((a.out_width + 255) / 256);
   if (tiles <= 128 || a.rows / a.E < 100) return launch_tiles<kBwdW, 128, 128, 2, 2, 32, 3, TOKENS>(a, st);
   // gathered rows: longer steps, which fetch their tokens half as often
   if constexpr (TOKENS)
@@ -656,7 +663,7 @@ hipError_t launch_bwd_w(const ExpertArgs& a, hipStream_t st) {
 
 hipError_t launch_experts_fwd(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_fwd", st);
-  return launch_rows_of<kFwd>(a, a.out_width, a.b2 != nullptr ? 2 : 1, st);
+  return launch_rows_of<kFwd>(a, a.out_width, pairs<kFwd>(a), st);
 }
 hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("experts_bwd_x", st);

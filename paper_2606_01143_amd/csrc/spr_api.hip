@@ -1771,8 +1771,8 @@ spr_status spr_experts_fwd(int32_t n_experts, int32_t rows, int32_t in_width, in
                            const void* w, void* y, const void* w2, void* y2, hipStream_t stream) {
   spr_status st = check_products(n_experts, rows, in_width, out_width, row_token != nullptr, x_rows);
   if (st != SPR_OK) return st;
-  if ((st = check_pair("w2 and y2", w2, y2)) != SPR_OK) return st;
   if (rows == 0) return ok();
+  if ((st = check_pair("w2 and y2", w2, y2)) != SPR_OK) return st;
   const size_t wb = (size_t)n_experts * in_width * out_width * 2, yb = (size_t)rows * out_width * 2;
   const std::vector<Buf> bufs = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
                                  {x, (size_t)x_rows * in_width * 2, "x", true},
@@ -1798,8 +1798,8 @@ spr_status spr_experts_bwd_x(int32_t n_experts, int32_t rows, int32_t in_width, 
                              void* dx, hipStream_t stream) {
   spr_status st = check_products(n_experts, rows, in_width, out_width, false, rows);
   if (st != SPR_OK) return st;
-  if ((st = check_pair("dy2 and w2", dy2, w2)) != SPR_OK) return st;
   if (rows == 0) return ok();
+  if ((st = check_pair("dy2 and w2", dy2, w2)) != SPR_OK) return st;
   const size_t wb = (size_t)n_experts * in_width * out_width * 2, yb = (size_t)rows * out_width * 2;
   const std::vector<Buf> bufs = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
                                  {dy, yb, "dy", true}, {w, wb, "w", true}, {dy2, yb, "dy2", false},
@@ -1822,8 +1822,9 @@ spr_status spr_experts_bwd_w(int32_t n_experts, int32_t rows, int32_t in_width, 
                              hipStream_t stream) {
   spr_status st = check_products(n_experts, rows, in_width, out_width, row_token != nullptr, x_rows);
   if (st != SPR_OK) return st;
-  if ((st = check_pair("dy2 and dw2", dy2, dw2)) != SPR_OK) return st;
   if (rows == 0 && overwrite == 0) return ok();
+  // without rows dy2 may be NULL, as an empty tensor's pointer is
+  if (rows > 0 && (st = check_pair("dy2 and dw2", dy2, dw2)) != SPR_OK) return st;
   const size_t wb = (size_t)n_experts * in_width * out_width * 4, yb = (size_t)rows * out_width * 2;
   const std::vector<Buf> bufs = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", true, 4},
                                  {x, rows ? (size_t)x_rows * in_width * 2 : 0, "x", true},

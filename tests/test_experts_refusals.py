@@ -99,6 +99,13 @@ def test_nothing_to_do_launches_nothing():
     assert _call("spr_experts_combine_bwd", COMBINE_BWD, T=0) == "SPR_OK"
 
 
+def test_no_rows_of_a_pair():
+    """An empty tensor's pointer is NULL: no half of a pair is missing."""
+    assert _call("spr_experts_fwd", FWD, rows=0, x=None, y=None, y2=None) == "SPR_OK"
+    assert _call("spr_experts_bwd_x", BWD_X, rows=0, dy=None, dy2=None, dx=None) == "SPR_OK"
+    assert _call("spr_experts_bwd_w", BWD_W, rows=0, x=None, dy=None, dy2=None, overwrite=0) == "SPR_OK"
+
+
 def test_plan_workspace_size():
     assert B.experts_plan_workspace_size(8, 2, 2048) == 0
     mid, large = B.experts_plan_workspace_size(8, 2, 2049), B.experts_plan_workspace_size(1024, 8, 1 << 20)

@@ -130,6 +130,23 @@ def test_no_rows(gpu):
     _check_all(s, 16, 24)
 
 
+def test_no_rows_of_a_pair(gpu):
+    import torch
+    from paper_2606_01143_amd import binding as B
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    off, w = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.randn(4, 16, 24, device="cuda").bfloat16()
+    x, dy, tokens = torch.empty(0, 16, **bf), torch.empty(0, 24, **bf), torch.empty(0, dtype=torch.int32, device="cuda")
+    table = torch.ones(7, 16, **bf)
+    for src, rt in ((x, None), (table, tokens)):
+        B.experts_fwd(off, src, w, torch.empty(0, 24, **bf), w, torch.empty(0, 24, **bf), row_token=rt)
+        dw, dw2 = torch.ones(4, 16, 24, device="cuda"), torch.ones(4, 16, 24, device="cuda")
+        B.experts_bwd_w(off, src, dy, dw, dy, dw2, row_token=rt)
+        assert (dw == 1).all() and (dw2 == 1).all()
+        B.experts_bwd_w(off, src, dy, dw, dy, dw2, row_token=rt, overwrite=True)
+        assert (dw == 0).all() and (dw2 == 0).all()
+    B.experts_bwd_x(off, dy, w, x, dy, w)
+
+
 def test_a_bad_row_stays_in_its_group(gpu):
     """NaN and infinity in one expert's last row, its weights or the rows
     behind the last group reach nothing else; ragged contraction ends too."""
