@@ -41,7 +41,8 @@ spr_status spr_rope_bwd(int32_t tokens, int32_t heads, int32_t head_dim, int32_t
 
 /* RMSNorm of every query and key head with a gain, and the rotary embedding,
  * in one pass (layers that normalise their heads before attention):
- *   z = x g / sqrt(mean(x^2) + eps) over the head's d values, y = R z,
+ *   z = x g / sqrt(mean(x^2) + eps) over the head's d values (summed in fp32),
+ *   y = R z,
  * with R the rotation of spr_rope_fwd at position pos0 + positions[t]
  * (positions: DEVICE int32 [tokens], any values), or pos0 + t where
  * `positions` is NULL.  Packed suffixes, which all start behind one prefix,

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kHeadThreads) void head_norm_rope_bwd_kernel(HeadAr
       }
     }
     const float r = rsqrtf(wave_sum(ss) / (float)a.d + a.eps);
-    const float k3 = r * r * r * (wave_sum(dot) / (float)a.d);
+    const float k3 = r * (r * (r * (wave_sum(dot) / (float)a.d)));  // r^3 alone can pass the range
 #pragma unroll
     for (int c = 0; c < kMaxPairs; ++c) {
       const int j = lane + 64 * c, i = 2 * c;
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kHeadThreads) void head_rows_bwd_kernel(HeadArgs a,
       dot = fmaf(d0[j] * g.lo.at(j), x.lo.at(j), fmaf(d1[j] * g.hi.at(j), x.hi.at(j), dot));
     }
     const float rs = rsqrtf(group_sum<G>(ss) / (float)a.d + a.eps);
-    const float k3 = rs * rs * rs * (group_sum<G>(dot) / (float)a.d);
+    const float k3 = rs * (rs * (rs * (group_sum<G>(dot) / (float)a.d)));  // rs^3 alone can pass the range
     const int h = r.first + lane / G;
     if (col < half && h < r.heads) {
       T* dx = (r.is_q ? (T*)a.dq + r.t * a.dq_stride : (T*)a.dk + r.t * a.dk_stride) + h * a.d + col;

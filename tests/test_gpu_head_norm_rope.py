@@ -116,6 +116,14 @@ def test_against_the_formulas(gpu, T, hq, hkv, d, dt, extra, lead):
     assert torch.equal(rest, torch.full_like(rest, 7.0))
 
 
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("bf16", 72), ("f32", 64), ("f32", 72)])
+def test_small_rows_without_eps(gpu, dt, d):
+    """Rows whose 1 / rms has a cube beyond fp32's range, but no gradient has."""
+    i = _inputs(9, 3, 2, d, _dt(dt), seed=d)
+    i["x"].mul_(2.0 ** -48)
+    _check(i, _run(i, 5, 0.0), 5 + np.arange(9), 0.0)
+
+
 @pytest.mark.parametrize("dt,d", [("bf16", 128), ("f32", 64), ("bf16", 72)])
 def test_positions(gpu, dt, d):
     """Packed suffixes, a repeated and a negative position, and far ones."""
