@@ -33,69 +33,72 @@ __global__ __launch_bounds__(kSortThreads) void experts_plan_kernel(SortPass p, 
   });
 }
 
-// one workgroup per token, eight values a thread
+// a workgroup per token, eight values a thread
 __global__ __launch_bounds__(kRowThreads) void combine_fwd_kernel(const bf16* __restrict__ y,
                                                                   const int* __restrict__ pos,
                                                                   const float* __restrict__ weights, const bf16* add,
-                                                                  bf16* out, int k, int rows, int chunks) {
-  const long t = blockIdx.x;
-  for (int c = threadIdx.x; c < chunks; c += kRowThreads) {
-    float sum[8] = {};
-    for (int j = 0; j < k; ++j) {
-      const int p = pos[t * k + j];
-      if ((unsigned)p >= (unsigned)rows) continue;
-      const float w = weights ? weights[t * k + j] : 1.f;
-      float v[8];
-      load8(y + ((long)p * chunks + c) * 8, v);
+                                                                  bf16* out, long tokens, int k, int rows,
+                                                                  int chunks) {
+  for (long t = blockIdx.x; t < tokens; t += gridDim.x) {
+    for (int c = threadIdx.x; c < chunks; c += kRowThreads) {
+      float sum[8] = {};
+      for (int j = 0; j < k; ++j) {
+        const int p = pos[t * k + j];
+        if ((unsigned)p >= (unsigned)rows) continue;
+        const float w = weights ? weights[t * k + j] : 1.f;
+        float v[8];
+        load8(y + ((long)p * chunks + c) * 8, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
-    }
-    const long at = (t * chunks + c) * 8;
-    if (add) {
-      float v[8];
-      load8(add + at, v);
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+      }
+      const long at = (t * chunks + c) * 8;
+      if (add) {
+        float v[8];
+        load8(add + at, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+      }
+      store8(out + at, sum);
     }
-    store8(out + at, sum);
   }
 }
 
-// one wave per choice
+// a wave per choice
 __global__ __launch_bounds__(kRowThreads) void combine_bwd_kernel(const bf16* __restrict__ dout,
                                                                   const bf16* __restrict__ y,
                                                                   const int* __restrict__ pos,
                                                                   const float* __restrict__ weights,
                                                                   bf16* __restrict__ dy, float* __restrict__ dweights,
                                                                   long slots, int k, int rows, int chunks) {
-  const long i = (long)blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6);
+  constexpr int kWaves = kRowThreads / 64;
   const int lane = threadIdx.x & 63;
-  if (i >= slots) return;
-  const int p = pos[i];
-  if ((unsigned)p >= (unsigned)rows) {
-    if (dweights && lane == 0) dweights[i] = 0.f;
-    return;
-  }
-  const float w = weights ? weights[i] : 1.f;
-  const bf16* d = dout + i / k * chunks * 8;
-  float dot = 0.f;
-  for (int c = lane; c < chunks; c += 64) {
-    float g[8], o[8];
-    load8(d + 8 * c, g);
-    if (dweights) {
-      float v[8];
-      load8(y + ((long)p * chunks + c) * 8, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) dot = fmaf(v[j], g[j], dot);
+  for (long i = (long)blockIdx.x * kWaves + (threadIdx.x >> 6); i < slots; i += (long)gridDim.x * kWaves) {
+    const int p = pos[i];
+    if ((unsigned)p >= (unsigned)rows) {
+      if (dweights && lane == 0) dweights[i] = 0.f;
+      continue;
     }
+    const float w = weights ? weights[i] : 1.f;
+    const bf16* d = dout + i / k * chunks * 8;
+    float dot = 0.f;
+    for (int c = lane; c < chunks; c += 64) {
+      float g[8], o[8];
+      load8(d + 8 * c, g);
+      if (dweights) {
+        float v[8];
+        load8(y + ((long)p * chunks + c) * 8, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = w * g[j];
-    store8(dy + ((long)p * chunks + c) * 8, o);
-  }
-  if (dweights) {
+        for (int j = 0; j < 8; ++j) dot = fmaf(v[j], g[j], dot);
+      }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
-    if (lane == 0) dweights[i] = dot;
+      for (int j = 0; j < 8; ++j) o[j] = w * g[j];
+      store8(dy + ((long)p * chunks + c) * 8, o);
+    }
+    if (dweights) {
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) dot += __shfl_xor(dot, o);
+      if (lane == 0) dweights[i] = dot;
+    }
   }
 }
 
@@ -118,8 +121,8 @@ hipError_t launch_combine_fwd(int tokens, int k, int rows, int width, const void
                               const float* weights, const void* add, void* out, hipStream_t st) {
   if (tokens == 0) return hipSuccess;
   ProfileScope ps("experts_combine_fwd", st);
-  hipLaunchKernelGGL(combine_fwd_kernel, dim3(tokens), dim3(kRowThreads), 0, st, (const bf16*)y, pos, weights,
-                     (const bf16*)add, (bf16*)out, k, rows, width / 8);
+  hipLaunchKernelGGL(combine_fwd_kernel, dim3(grid_of(tokens, kRowThreads)), dim3(kRowThreads), 0, st, (const bf16*)y, pos,
+                     weights, (const bf16*)add, (bf16*)out, (long)tokens, k, rows, width / 8);
   return hipGetLastError();
 }
 
@@ -128,7 +131,7 @@ hipError_t launch_combine_bwd(int tokens, int k, int rows, int width, const void
   const long slots = (long)tokens * k;
   if (slots == 0) return hipSuccess;
   ProfileScope ps("experts_combine_bwd", st);
-  hipLaunchKernelGGL(combine_bwd_kernel, dim3((unsigned)((slots + 3) / 4)), dim3(kRowThreads), 0, st,
+  hipLaunchKernelGGL(combine_bwd_kernel, dim3(grid_of((slots + 3) / 4, kRowThreads)), dim3(kRowThreads), 0, st,
                      (const bf16*)dout, (const bf16*)y, pos, weights, (bf16*)dy, dweights, slots, k, rows, width / 8);
   return hipGetLastError();
 }

@@ -50,17 +50,18 @@ template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_fwd_kernel(const int* __restrict__ ids,
                                                                   const T* __restrict__ table, T* __restrict__ y,
                                                                   long tokens, int vocab, int chunks, float scale) {
-  const long i = (long)blockIdx.x * kEmbedThreads + threadIdx.x;
-  if (i >= tokens * chunks) return;
-  const long t = i / chunks, c = i % chunks;
-  const int id = ids[t];
-  float v[8] = {};
-  if ((unsigned)id < (unsigned)vocab) {
-    Vec8<T>::load(table + ((long)id * chunks + c) * 8, v);
+  for (long i = (long)blockIdx.x * kEmbedThreads + threadIdx.x; i < tokens * chunks;
+       i += (long)gridDim.x * kEmbedThreads) {
+    const long t = i / chunks, c = i % chunks;
+    const int id = ids[t];
+    float v[8] = {};
+    if ((unsigned)id < (unsigned)vocab) {
+      Vec8<T>::load(table + ((long)id * chunks + c) * 8, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= scale;
+      for (int j = 0; j < 8; ++j) v[j] *= scale;
+    }
+    Vec8<T>::store(y + 8 * i, v);
   }
-  Vec8<T>::store(y + 8 * i, v);
 }
 
 // Up to kFewTokens tokens: no sort and one launch.  The wave of a token and 512
@@ -334,7 +335,7 @@ hipError_t launch_embed_fwd(int dtype, int tokens, int vocab, int width, float s
   const long n = (long)tokens * (width / 8);
   if (n == 0) return hipSuccess;
   ProfileScope ps("embed_fwd", st);
-  const dim3 grid((unsigned)((n + kEmbedThreads - 1) / kEmbedThreads));
+  const dim3 grid(grid_of((n + kEmbedThreads - 1) / kEmbedThreads, kEmbedThreads));
   if (dtype == 1)
     hipLaunchKernelGGL(embed_fwd_kernel<bf16>, grid, dim3(kEmbedThreads), 0, st, ids, (const bf16*)table, (bf16*)y,
                        (long)tokens, vocab, width / 8, scale);

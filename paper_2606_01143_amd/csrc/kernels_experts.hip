@@ -599,7 +599,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
     grid = (MODE == kFwd ? parts : 1) * tiles_n * ((a.rows + some * (BM - 1)) / BM);
   }
   grid = (grid + kXcds - 1) / kXcds * kXcds;
-  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (grid * (64L * MW * NW) > (long)UINT32_MAX) return hipErrorInvalidConfiguration;  // threads of a launch
   if (grid == 0) return hipSuccess;
   hipLaunchKernelGGL((experts_kernel<MODE, BM, BN, MW, NW, STEP, RING, TOKENS>), dim3((unsigned)grid), dim3(64 * MW * NW),
                      0, st, a);

@@ -41,37 +41,38 @@ __device__ __forceinline__ double head_pos(const HeadArgs& a, long t) {
 }  // namespace
 
 // ------------------------------------------------ any head dim and alignment
-// One wave per row; lane l has the pairs l and l + 64.
+// A wave per row; lane l has the pairs l and l + 64.
 template <typename T>
 __global__ __launch_bounds__(kHeadThreads) void head_norm_rope_fwd_kernel(HeadArgs a) {
   const int lane = threadIdx.x & 63, heads = a.hq + a.hkv, half = a.d / 2;
-  const long row = (long)blockIdx.x * kHeadWaves + (threadIdx.x >> 6);
-  if (row >= (long)a.tokens * heads) return;
-  const long t = row / heads;
-  const int h = (int)(row % heads);
-  const bool is_q = h < a.hq;
-  const int hh = is_q ? h : h - a.hq;
-  const T* x = is_q ? (const T*)a.q + t * a.q_stride + (long)hh * a.d : (const T*)a.k + t * a.k_stride + (long)hh * a.d;
-  T* y = is_q ? (T*)a.yq + (t * a.hq + hh) * a.d : (T*)a.yk + (t * a.hkv + hh) * a.d;
-  const T* g = (const T*)(is_q ? a.gain_q : a.gain_k);
-  float u[kMaxPairs], v[kMaxPairs], ss = 0.f;
+  const long rows = (long)a.tokens * heads;
+  for (long row = (long)blockIdx.x * kHeadWaves + (threadIdx.x >> 6); row < rows; row += (long)gridDim.x * kHeadWaves) {
+    const long t = row / heads;
+    const int h = (int)(row % heads);
+    const bool is_q = h < a.hq;
+    const int hh = is_q ? h : h - a.hq;
+    const T* x = is_q ? (const T*)a.q + t * a.q_stride + (long)hh * a.d : (const T*)a.k + t * a.k_stride + (long)hh * a.d;
+    T* y = is_q ? (T*)a.yq + (t * a.hq + hh) * a.d : (T*)a.yk + (t * a.hkv + hh) * a.d;
+    const T* g = (const T*)(is_q ? a.gain_q : a.gain_k);
+    float u[kMaxPairs], v[kMaxPairs], ss = 0.f;
 #pragma unroll
-  for (int c = 0; c < kMaxPairs; ++c) {
-    const int j = lane + 64 * c;
-    u[c] = j < half ? to_f32(x[j]) : 0.f;
-    v[c] = j < half ? to_f32(x[j + half]) : 0.f;
-    ss = fmaf(u[c], u[c], fmaf(v[c], v[c], ss));
-  }
-  const float r = rsqrtf(wave_sum(ss) / (float)a.d + a.eps);
-  const double pos = head_pos(a, t);
+    for (int c = 0; c < kMaxPairs; ++c) {
+      const int j = lane + 64 * c;
+      u[c] = j < half ? to_f32(x[j]) : 0.f;
+      v[c] = j < half ? to_f32(x[j + half]) : 0.f;
+      ss = fmaf(u[c], u[c], fmaf(v[c], v[c], ss));
+    }
+    const float r = rsqrtf(wave_sum(ss) / (float)a.d + a.eps);
+    const double pos = head_pos(a, t);
 #pragma unroll
-  for (int c = 0; c < kMaxPairs; ++c) {
-    const int j = lane + 64 * c;
-    if (j < half) {
-      const float2 w = head_angle(pos, j, a);
-      const float p = u[c] * r * to_f32(g[j]), q = v[c] * r * to_f32(g[j + half]);
-      y[j] = from_f32<T>(p * w.x - q * w.y);
-      y[j + half] = from_f32<T>(q * w.x + p * w.y);
+    for (int c = 0; c < kMaxPairs; ++c) {
+      const int j = lane + 64 * c;
+      if (j < half) {
+        const float2 w = head_angle(pos, j, a);
+        const float p = u[c] * r * to_f32(g[j]), q = v[c] * r * to_f32(g[j + half]);
+        y[j] = from_f32<T>(p * w.x - q * w.y);
+        y[j + half] = from_f32<T>(q * w.x + p * w.y);
+      }
     }
   }
 }
@@ -526,7 +527,7 @@ hipError_t launch_head_norm_rope_fwd(int dtype, const HeadArgs& a, hipStream_t s
       launch_rows<float, false>(a, (unsigned)blocks, parts, st);
     return hipGetLastError();
   }
-  const dim3 grid((unsigned)((rows + kHeadWaves - 1) / kHeadWaves));
+  const dim3 grid(grid_of((rows + kHeadWaves - 1) / kHeadWaves, kHeadThreads));
   if (dtype == 1)
     hipLaunchKernelGGL(head_norm_rope_fwd_kernel<bf16>, grid, dim3(kHeadThreads), 0, st, a);
   else

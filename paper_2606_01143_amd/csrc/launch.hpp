@@ -176,6 +176,13 @@ hipError_t launch_swiglu_bwd(long n, const void* g, const void* u, const void* d
 
 hipError_t launch_grad_accumulate(long n, const void* src, float* dst, bool overwrite, hipStream_t st);
 
+// Workgroups of a kernel whose n work items (one a workgroup) lie `gridDim`
+// apart: a launch has fewer than 2^32 threads.
+inline unsigned grid_of(long n, int threads) {
+  const long most = (1L << 31) / threads;
+  return (unsigned)(n < most ? n : most);
+}
+
 // per-head norm and rotation (kernels_heads.hip); strides in elements
 struct HeadArgs {
   const void* q;

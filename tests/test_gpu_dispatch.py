@@ -124,6 +124,27 @@ def test_combine_ignores_skipped_rows_values(gpu):
     assert dw[0, 0] == 32 and dw[0, 1] == 0 and (dy[3:] == 0).all()
 
 
+def test_more_choices_than_a_launch_has_waves(gpu):
+    """Small whole numbers: every sum and rounding is exact."""
+    import torch
+    from paper_2606_01143_amd import binding as B
+    T, k, width = (1 << 23) + 7, 4, 8
+    R = T * k
+    _say(f"combine T {T} k {k} width {width}")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    whole = lambda *s: torch.randint(-8, 9, s, generator=g, device="cuda", dtype=torch.int8)
+    y, dout, w = whole(R, width).bfloat16(), whole(T, width).bfloat16(), whole(T, k).float() / 2
+    pos = torch.arange(R - 1, -1, -1, dtype=torch.int32, device="cuda").view(T, k)
+    out = torch.empty(T, width, dtype=torch.bfloat16, device="cuda")
+    B.experts_combine_fwd(y, pos, w, out)
+    mine = y.flip(0).view(T, k, width)
+    assert torch.equal(out, (w[..., None] * mine).sum(1).bfloat16())
+    dy, dw = torch.empty_like(y), torch.empty_like(w)
+    B.experts_combine_bwd(dout, y, pos, w, dy, dw)
+    assert torch.equal(dw, (mine.float() * dout.float()[:, None]).sum(-1))
+    assert torch.equal(dy.flip(0).view(T, k, width), (w[..., None] * dout[:, None]).bfloat16())
+
+
 def test_no_tokens(gpu):
     import torch
     from paper_2606_01143_amd import binding as B

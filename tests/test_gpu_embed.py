@@ -139,6 +139,27 @@ def test_a_bad_row_reaches_its_own_id(gpu):
     assert t.sum() == 24
 
 
+def test_more_values_than_a_launch_has_threads_for(gpu):
+    """An output of 34 GB."""
+    import torch
+    from paper_2606_01143_amd import binding as B
+    T, width = (1 << 18) + 3, 65536
+    _say(f"fwd T {T} width {width}")
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    table = torch.randn(4, width, generator=g, device="cuda").bfloat16()
+    ids = torch.randint(-1, 4, (T,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.empty(T, width, dtype=torch.bfloat16, device="cuda")
+    B.embed_fwd(ids, table, y, scale=0.5)   # a power of two: no rounding
+    padded = torch.cat([table * 0.5, torch.zeros_like(table[:1])])
+    for at in range(0, T, 1 << 13):
+        part = y[at:at + (1 << 13)]
+        assert torch.equal(part, padded[ids[at:at + (1 << 13)].long()]), f"rows {at} on"
+    del y, part
+    torch.cuda.empty_cache()
+
+
 def test_no_tokens(gpu):
     import torch
     from paper_2606_01143_amd import binding as B

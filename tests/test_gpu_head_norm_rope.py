@@ -124,6 +124,23 @@ def test_small_rows_without_eps(gpu, dt, d):
     _check(i, _run(i, 5, 0.0), 5 + np.arange(9), 0.0)
 
 
+def test_more_rows_than_a_launch_has_waves(gpu):
+    import torch
+    from paper_2606_01143_amd import binding as B
+    T = (1 << 24) + 5
+    _say(f"T {T} heads 1/1 d 2")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    q, k, gq, gk = r(T, 1, 2), r(T, 1, 2), r(2), r(2)
+    yq, yk = torch.zeros_like(q), torch.zeros_like(k)
+    B.head_norm_rope_fwd(q, k, gq, gk, yq, yk, 0, THETA)
+    for at in (slice(0, 5), slice(T // 2, T // 2 + 9), slice(T - 30, T)):
+        pos = np.arange(at.start, at.stop, dtype=np.float64)
+        for x, gain, y in ((q, gq, yq), (k, gk, yk)):
+            ref, tol = _ref(x[at], gain, x[at], pos, 1e-6)[:2]
+            _close(y[at], ref, tol, f"y at {at}")
+
+
 @pytest.mark.parametrize("dt,d", [("bf16", 128), ("f32", 64), ("bf16", 72)])
 def test_positions(gpu, dt, d):
     """Packed suffixes, a repeated and a negative position, and far ones."""
