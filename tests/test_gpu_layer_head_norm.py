@@ -72,3 +72,35 @@ def test_gains_go_together():
     del inp["weights"]["gk"]
     with pytest.raises(ValueError, match="go together"):
         DecoderLayer(inp, device="cpu")
+
+
+@pytest.mark.gpu
+def test_from_the_embedding_and_back(gpu):
+    """Token ids -> embedding -> the layer's schedule -> the table's gradient, the
+    prefix's part once plus every suffix's.  A row of it adds its tokens' dx, each
+    within the layer's gate of its part's largest."""
+    from paper_2606_01143_amd import binding as B
+    from paper_2606_01143_amd.layer import DecoderLayer
+    shape, V = LayerShape(256, 4, 2, 64, 512, 300, (70, 33, 1)), 97
+    print(f"\n[gpu layer head norm] embedding of {V} ids, {shape}", flush=True)
+    inp, g = _group(shape, seed=6), torch.Generator().manual_seed(6)
+    table = torch.randn(V, 256, generator=g).bfloat16().cuda()
+    ids = [torch.randint(0, V, (n,), generator=g, dtype=torch.int32).cuda() for n in (300, 70, 33, 1)]
+    x = [torch.empty(len(t), 256, dtype=torch.bfloat16, device="cuda") for t in ids]
+    for t, to in zip(ids, x):
+        B.embed_fwd(t, table, to)
+        assert torch.equal(to, table[t.long()])
+    host = [t.float().cpu().numpy() for t in x]
+    inp["x_p"], inp["x_s"] = host[0], host[1:]
+    got, ref = DecoderLayer(inp).run_schedule(), _reference(inp)
+    dtable = torch.zeros(V, 256, device="cuda")
+    want, tol = np.zeros((V, 256)), np.zeros((V, 1))
+    for t, dx, r in zip(ids, [got["dx_p"], *got["dx_s"]], [ref["dx_p"], *ref["dx_s"]]):
+        ws = torch.empty(B.embed_bwd_workspace_size(len(t), V, 256), dtype=torch.uint8, device="cuda")
+        B.embed_bwd(t, dx.bfloat16().contiguous(), dtable, ws=ws)
+        at = t.cpu().numpy()
+        np.add.at(want, at, r)
+        # rounding dx to bf16, if it is not already, is 2^-8 of it more
+        np.add.at(tol, at, np.full((len(at), 1), (TOL + 2.0 ** -8) * np.abs(r).max()))
+    off = np.abs(dtable.double().cpu().numpy() - want) - tol
+    assert off.max() <= 0, off.max()
