@@ -122,28 +122,33 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const int* __r
 }
 
 // Up to kRankTokens tokens: a token's place is the number of keys that sort
-// before it, counted by eight lanes (two radix passes take two launches).
-constexpr int kRankTokens = 4096, kRankLanes = 8;
+// before it, counted by 32 lanes.  One launch, where a radix pass takes two.
+// Whole call of width 1024, us, by counting / in radix passes: 4096 tokens 23 /
+// 31, 8192 31 / 39, 12000 46 / 44.  (Eight lanes a token: 32 and 51.)
+constexpr int kRankTokens = 8192, kRankLanes = 32, kRankThreads = 1024;
 
-__global__ __launch_bounds__(kEmbedThreads) void embed_rank_kernel(const int* __restrict__ ids, int tokens, int vocab,
-                                                                   int* __restrict__ keys_out,
-                                                                   int* __restrict__ tokens_out) {
-  __shared__ unsigned keys[kRankTokens];
+__global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int* __restrict__ ids, int tokens, int vocab,
+                                                                  int* __restrict__ keys_out,
+                                                                  int* __restrict__ tokens_out) {
+  __shared__ __attribute__((aligned(16))) unsigned keys[kRankTokens];
   // whole rounds of 4 keys a lane; the places behind the last token sort last
   const int round = 4 * kRankLanes, padded = (tokens + round - 1) / round * round;
-  for (int i = threadIdx.x; i < padded; i += kEmbedThreads)
+#pragma unroll 4
+  for (int i = threadIdx.x; i < padded; i += kRankThreads)
     keys[i] = i < tokens ? (unsigned)sort_key(ids[i], vocab) : 0xffffffffu;
   __syncthreads();
-  const int mine = blockIdx.x * (kEmbedThreads / kRankLanes) + threadIdx.x / kRankLanes, part = threadIdx.x % kRankLanes;
+  const int mine = blockIdx.x * (kRankThreads / kRankLanes) + threadIdx.x / kRankLanes, part = threadIdx.x % kRankLanes;
   if (mine >= tokens) return;
   const unsigned key = keys[mine];
+  // smaller keys, and equal ones of earlier quads; then those of its own quad
   int before = 0;
 #pragma unroll 4
   for (int j = 4 * part; j < padded; j += round) {
     const uint4 k = *(const uint4*)(keys + j);
-    before += (k.x < key + (j < mine)) + (k.y < key + (j + 1 < mine)) + (k.z < key + (j + 2 < mine)) +
-              (k.w < key + (j + 3 < mine));
+    const unsigned bound = key + (j + 4 <= mine);
+    before += (k.x < bound) + (k.y < bound) + (k.z < bound) + (k.w < bound);
   }
+  if (part < mine % 4) before += keys[mine / 4 * 4 + part] == key;
 #pragma unroll
   for (int o = 1; o < kRankLanes; o <<= 1) before += __shfl_xor(before, o);
   if (part == 0) {
@@ -302,7 +307,7 @@ namespace {
 // from 8 to the 64 that a wave holds keys of.  Short spans cross more runs, whose
 // parts are written and read again; long ones leave CUs idle.  Whole call, us,
 // with 2048 / 4096 / 8192 waves as the aim, width 4096: 28672 tokens 179 / 163 /
-// 178, 8192 tokens 87 / 73 / 75, 28672 tokens of 500 ids 91 / 83 / 94.
+// 178, 8192 tokens 80 / 65 / 68, 28672 tokens of 500 ids 91 / 84 / 95.
 int embed_span(long n, long slabs) {
   int len = 8;
   while (len < 64 && 2 * len * 4096L <= n * slabs) len *= 2;
@@ -373,8 +378,8 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
   int out = 0;
   if (n <= kRankTokens) {
     ProfileScope ps("embed_rank", st);
-    constexpr int per_block = kEmbedThreads / kRankLanes;
-    hipLaunchKernelGGL(embed_rank_kernel, dim3((tokens + per_block - 1) / per_block), dim3(kEmbedThreads), 0, st, ids,
+    constexpr int per_block = kRankThreads / kRankLanes;
+    hipLaunchKernelGGL(embed_rank_kernel, dim3((tokens + per_block - 1) / per_block), dim3(kRankThreads), 0, st, ids,
                        tokens, vocab, keys[0], order[0]);
     k_in = keys[0];
     t_in = order[0];

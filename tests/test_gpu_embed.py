@@ -58,6 +58,8 @@ CASES = [(1, 7, 8, "any", "bf16"), (5, 1, 64, "one", "f32"), (64, 100, 520, "any
          # either side of the count in a launch of its own, and many spans of one id
          (4096, 700, 8, "frequent", "f32"), (65537, 700, 8, "frequent", "f32"), (33, 5, 8, "one", "bf16"),
          (32, 5, 8, "few", "f32"), (40000, 100, 72, "padded", "bf16"),
+         (8192, 900, 8, "frequent", "bf16"), (8191, 128000, 8, "any", "f32"), (8190, 50, 24, "padded", "bf16"),
+         (8193, 900, 8, "frequent", "f32"), (5000, 6, 8, "one", "bf16"), (7777, 7, 8, "dropped", "f32"),
          # the direct form's last size, ranks by counting up to theirs, and a row's ids in any part
          (256, 40, 520, "padded", "bf16"), (256, 3, 8, "one", "f32"), (255, 200, 1032, "any", "f32"),
          (257, 20, 520, "frequent", "bf16"), (4095, 2147483, 8, "padded", "f32"), (4097, 50, 24, "few", "bf16")]
