@@ -23,7 +23,8 @@
  * weights, which adds up each token's k rows.
  *
  * Conventions: 1 <= n_experts <= 1024; 1 <= top_k <= n_experts; n_tokens *
- * top_k <= 2^31 - 1.  Tensors are bf16, the router's weights, their gradients
+ * top_k <= 2^31 - 1; the products take at most 2^31 - 1025 rows, and widths of
+ * as much.  Tensors are bf16, the router's weights, their gradients
  * and the weight gradients fp32, all sums fp32.  Row-major, contiguous, device
  * memory owned by the caller, 16-byte aligned (int32 and the router's fp32
  * arrays: 4-byte).  Outputs overlap nothing unless a call says so.

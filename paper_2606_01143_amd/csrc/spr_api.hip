@@ -1716,6 +1716,10 @@ spr_status check_products(int32_t E, int32_t rows, int32_t in_width, int32_t out
   if ((st = check_width("out_width", out_width)) != SPR_OK) return st;
   if (rows > 0 && x_rows < (gathers ? 1 : rows))
     return fail(SPR_ERR_INVALID_ARG, gathers ? "x_rows must be >= 1" : "x_rows must be >= rows without row_token");
+  // the kernels round rows and widths up to whole tiles and steps of 256 at most,
+  // and look a ring of steps (256 indices) ahead, in 32 bits
+  if (rows > INT32_MAX - 1024 || in_width > INT32_MAX - 1024 || out_width > INT32_MAX - 1024)
+    return fail(SPR_ERR_INVALID_ARG, "rows and widths must be at most 2^31 - 1025");
   // the launch's tiles: 32 rows and 32 columns each at the least
   if (((int64_t)rows / 32 + E) * (2 * ((int64_t)(in_width > out_width ? in_width : out_width) / 32 + 1)) > INT32_MAX ||
       (int64_t)E * 2 * (in_width / 32 + 1) * (out_width / 32 + 1) > INT32_MAX)

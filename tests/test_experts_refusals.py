@@ -142,3 +142,26 @@ def test_binding_types_and_shapes():
         B.experts_combine_fwd(y, i32(5, 2), bf(5, 2), bf(5, 24))
     with pytest.raises(ValueError, match="dweights: shape"):
         B.experts_combine_bwd(bf(5, 24), y, i32(5, 2), None, y, torch.zeros(5, 1))
+
+
+# sizes that 32 bits hold, but not what the kernels round them up to
+@pytest.mark.parametrize("kw", [dict(rows=2147483647, x_rows=2147483647, i=8, o=8), dict(rows=2147483400, x_rows=2147483400, i=8, o=8),
+                                dict(rows=2147482624, x_rows=2147482624, i=8, o=8),
+                                dict(E=1, rows=1, i=2147483640, o=8), dict(E=1, rows=1, i=8, o=2147482624)])
+def test_sizes_next_to_32_bits(kw):
+    far = lambda *names: {n: 0x7F0000000000 + j * (1 << 40) for j, n in enumerate(names)}
+    plain = {k: v for k, v in kw.items() if k != "x_rows"}
+    for call, base, args in (("spr_experts_fwd", FWD, {**kw, **far("x", "w", "y", "w2", "y2", "offsets")}),
+                             ("spr_experts_bwd_x", BWD_X, {**plain, **far("dy", "w", "dy2", "w2", "dx", "offsets")}),
+                             ("spr_experts_bwd_w", BWD_W, {**kw, **far("x", "dy", "dw", "dy2", "dw2", "offsets")}),
+                             ("spr_experts_bwd_w", BWD_W, {**kw, **far("x", "dy", "dw", "dy2", "dw2", "offsets", "row_token")})):
+        assert _call(call, base, **args) == "SPR_ERR_INVALID_ARG", call
+        assert "2^31 - 1025" in B.last_error()
+
+
+def test_the_largest_widths_without_rows():
+    most = 2147482616
+    for i, o in ((most, 8), (8, most)):
+        assert _call("spr_experts_fwd", FWD, E=1, rows=0, i=i, o=o) == "SPR_OK"
+        assert _call("spr_experts_bwd_x", BWD_X, E=1, rows=0, i=i, o=o) == "SPR_OK"
+        assert _call("spr_experts_bwd_w", BWD_W, E=1, rows=0, i=i, o=o, overwrite=0) == "SPR_OK"
