@@ -92,7 +92,8 @@ spr_status spr_grad_accumulate(int64_t n, const void* src, float* dst, int32_t o
 /* Embedding lookup: y[t] = scale * table[ids[t]], y [tokens, width], table
  * [vocab, width], both of `dtype` (SPR_BF16 or SPR_F32); ids DEVICE int32
  * [tokens].  An id outside [0, vocab) (padding) gives a row of zeros.  width a
- * multiple of 8, any vocab >= 1. */
+ * multiple of 8, any vocab >= 1, tokens * width at most 2^39 (here and in the
+ * gradient). */
 spr_status spr_embed_fwd(int32_t dtype, int32_t tokens, int32_t vocab, int32_t width, float scale,
                          const int32_t* ids, const void* table, void* y, hipStream_t stream);
 

@@ -73,52 +73,55 @@ template <typename T>
 __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const int* __restrict__ ids,
                                                                   const T* __restrict__ dy, float* dtable, int tokens,
                                                                   int vocab, int chunks, int slabs, float scale) {
-  const int wave = blockIdx.x * (kEmbedThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = wave / slabs, lane = threadIdx.x & 63, chunk = wave % slabs * 64 + lane;
-  if (t >= tokens) return;
-  const int id = ids[t];
-  if ((unsigned)id >= (unsigned)vocab) return;
-  const bool in = chunk < chunks;
-  float* dst = dtable + ((long)id * chunks + chunk) * 8;
-  float old[8] = {}, sum[8] = {};
-  if (in) Vec8<float>::load(dst, old);
-  unsigned long long same[kFewTokens / 64];
+  constexpr int kWaves = kEmbedThreads / 64;
+  const int lane = threadIdx.x & 63;
+  for (long wave = (long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+       wave < (long)tokens * slabs; wave += (long)gridDim.x * kWaves) {
+    const int t = (int)wave / slabs, chunk = (int)wave % slabs * 64 + lane;
+    const int id = ids[t];
+    if ((unsigned)id >= (unsigned)vocab) continue;
+    const bool in = chunk < chunks;
+    float* dst = dtable + ((long)id * chunks + chunk) * 8;
+    float old[8] = {}, sum[8] = {};
+    if (in) Vec8<float>::load(dst, old);
+    unsigned long long same[kFewTokens / 64];
 #pragma unroll
-  for (int c = 0; c < kFewTokens / 64; ++c) {
-    const int j = 64 * c + lane;
-    same[c] = __ballot(j < tokens && ids[min(j, tokens - 1)] == id);
-  }
-  // the next of the id's tokens, or -1
-  auto next = [&]() -> int {
-    int at = -1;
-#pragma unroll
-    for (int c = kFewTokens / 64 - 1; c >= 0; --c)
-      if (same[c] != 0) at = 64 * c + __builtin_ctzll(same[c]);
-#pragma unroll
-    for (int c = 0; c < kFewTokens / 64; ++c)
-      if (at >= 0 && at >> 6 == c) same[c] &= same[c] - 1;
-    return at;
-  };
-  int row = next();
-  if (row != t) return;  // an earlier token's wave does it
-  while (row >= 0) {
-    float v[8][8] = {};
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      if (row >= 0) {
-        if (in) Vec8<T>::load(dy + ((long)row * chunks + chunk) * 8, v[q]);
-        row = next();
-      }
+    for (int c = 0; c < kFewTokens / 64; ++c) {
+      const int j = 64 * c + lane;
+      same[c] = __ballot(j < tokens && ids[min(j, tokens - 1)] == id);
     }
+    // the next of the id's tokens, or -1
+    auto next = [&]() -> int {
+      int at = -1;
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
+      for (int c = kFewTokens / 64 - 1; c >= 0; --c)
+        if (same[c] != 0) at = 64 * c + __builtin_ctzll(same[c]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += v[q][j];
+      for (int c = 0; c < kFewTokens / 64; ++c)
+        if (at >= 0 && at >> 6 == c) same[c] &= same[c] - 1;
+      return at;
+    };
+    int row = next();
+    if (row != t) continue;  // an earlier token's wave does it
+    while (row >= 0) {
+      float v[8][8] = {};
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (row >= 0) {
+          if (in) Vec8<T>::load(dy + ((long)row * chunks + chunk) * 8, v[q]);
+          row = next();
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += v[q][j];
+    }
+    if (!in) continue;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) old[j] = fmaf(scale, sum[j], old[j]);
+    Vec8<float>::store(dst, old);
   }
-  if (!in) return;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) old[j] = fmaf(scale, sum[j], old[j]);
-  Vec8<float>::store(dst, old);
 }
 
 // Up to kRankTokens tokens: a token's place is the number of keys that sort
@@ -357,7 +360,7 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
   if (n <= kFewTokens) {
     ProfileScope ps("embed_few", st);
     const int few_slabs = (width / 8 + 63) / 64;
-    const dim3 few_grid((unsigned)((n * few_slabs + kEmbedThreads / 64 - 1) / (kEmbedThreads / 64)));
+    const dim3 few_grid(grid_of((n * few_slabs + kEmbedThreads / 64 - 1) / (kEmbedThreads / 64), kEmbedThreads));
     if (dtype == 1)
       hipLaunchKernelGGL(embed_few_kernel<bf16>, few_grid, dim3(kEmbedThreads), 0, st, ids, (const bf16*)dy, dtable,
                          tokens, vocab, width / 8, few_slabs, scale);

@@ -1636,9 +1636,10 @@ spr_status check_embed(int32_t dtype, int32_t tokens, int32_t vocab, int32_t wid
   if (st != SPR_OK) return st;
   if (tokens < 0 || vocab < 1) return fail(SPR_ERR_INVALID_ARG, "tokens must be >= 0, vocab >= 1");
   if (width < 8 || width % 8 != 0) return fail(SPR_ERR_UNSUPPORTED, "width must be a positive multiple of 8");
-  // one launch covers a chunk of eight values per thread, 256 a workgroup
-  if ((int64_t)tokens * (width / 8) > ((int64_t)INT32_MAX << 8))
-    return fail(SPR_ERR_INVALID_ARG, "tokens * width exceeds 2^42");
+  // a terabyte in bf16, more than the card has; up to here the gradient's waves, one
+  // for 64 tokens and 512 columns, are fewer than the 2^26 of a launch
+  if ((int64_t)tokens * width > (int64_t)1 << 39)
+    return fail(SPR_ERR_INVALID_ARG, "tokens * width exceeds 2^39");
   if (!isfinite(scale)) return fail(SPR_ERR_INVALID_ARG, "scale must be finite");
   return SPR_OK;
 }

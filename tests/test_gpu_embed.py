@@ -202,3 +202,25 @@ def test_captured_and_on_another_stream(gpu):
             torch.cuda.synchronize()
             assert torch.equal(t, eager)
             (eager * 2).sum()
+
+
+def test_few_tokens_of_more_columns_than_a_launch_has_waves(gpu):
+    """256 tokens by 2^27 + 520 columns: a wave for a token and 512 columns would be
+    more than 2^32 threads.  Whole numbers, which fp32 adds exactly."""
+    import torch
+    T, V, width = 256, 2, (1 << 27) + 520
+    _say(f"bwd T {T} width {width}")
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    g = torch.Generator(device="cuda").manual_seed(7)
+    row = torch.randint(-4, 5, (width,), generator=g, device="cuda").bfloat16()
+    times = torch.randint(-3, 4, (T,), generator=g, device="cuda").bfloat16()
+    ids = torch.randint(-1, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    dy = torch.mul(times[:, None], row)
+    table = torch.ones(V, width, device="cuda")
+    _bwd(ids, dy, table, 0.5)
+    for v in range(V):
+        want = row.float() * (0.5 * times[ids == v].float().sum()) + 1
+        assert torch.equal(table[v], want), f"row {v}"
+    del dy, table, want
+    torch.cuda.empty_cache()

@@ -180,3 +180,10 @@ def test_binding_strides_and_device(monkeypatch):
     with pytest.raises(ValueError, match="the tensors are on cuda:1, not on the current device cuda:0"):
         B._on(1, 5)
     assert B._on(0, 5) == 5
+
+
+def test_embed_sizes_that_a_launch_holds():
+    """2^39 values are still taken (their NULL pointer is not), more are not."""
+    for fwd in (True, False):
+        assert _embed(fwd, T=1 << 27, w=4096, ids=None) == "SPR_ERR_INVALID_ARG" and "ids" in B.last_error()
+        assert _embed(fwd, T=(1 << 27) + 1, w=4096, ids=None) == "SPR_ERR_INVALID_ARG" and "2^39" in B.last_error()
