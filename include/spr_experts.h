@@ -29,8 +29,9 @@
  * memory owned by the caller, 16-byte aligned (int32 and the router's fp32
  * arrays: 4-byte).  Outputs overlap nothing unless a call says so.
  * `offsets` and `row_token` are read on the device: offsets are clamped into
- * [0, rows] and to be non-decreasing, tokens into [0, x_rows), so that wrong
- * values give wrong rows but no access outside the caller's buffers.  Calls
+ * [0, rows] and each raised to the largest one before it, tokens clamped into
+ * [0, x_rows), so that wrong values give wrong rows but no access outside the
+ * caller's buffers, and no row to two experts.  Calls
  * are asynchronous on `stream`; on a validation error nothing is launched and
  * spr_last_error() says why.  Every result is bitwise reproducible.
  */

@@ -210,17 +210,42 @@ struct GroupTile {
 // of experts a lane, and finds the range that holds t.
 // The workgroups of one XCD (blockIdx modulo 8) take consecutive tiles, which
 // share an expert's weights and rows in its L2.
+//
+// Group e is [M(e), M(e + 1)) with M the running maximum of the offsets, clamped
+// into [0, rows]: groups of any offsets at all are apart, and their tiles no more
+// than the launch has.  Offsets in order, as one ballot tells, are their own M.
 template <int BM>
 __device__ __forceinline__ GroupTile find_tile(const ExpertArgs& a, int cols, int lane) {
   const int per = (a.E + 63) / 64;
-  auto rows_of = [&](int e, int& lo) {
-    lo = clampi(a.offsets[e], 0, a.rows);
-    return clampi(a.offsets[e + 1], lo, a.rows) - lo;
+  auto offset = [&](int e) { return clampi(a.offsets[e], 0, a.rows); };
+  // tile rows of this lane's experts, and their last M; `lo`: M of the expert before
+  // them, or less where that is no larger than their first offset
+  auto count = [&](int lo, int& top, bool& sorted) {
+    const int e0 = lane * per;
+    int tiles = 0, first = offset(min(e0, a.E));
+    lo = max(lo, first);
+#pragma unroll 4
+    for (int q = 1; q <= per; ++q) {
+      const int next = offset(min(e0 + q, a.E)), hi = max(lo, next);
+      sorted &= next >= first;
+      tiles += (hi - lo + BM - 1) / BM;
+      lo = hi;
+      first = next;
+    }
+    top = lo;
+    return tiles;
   };
-  int mine = 0, lo;
-  for (int q = 0; q < per; ++q) {
-    const int e = lane * per + q;
-    if (e < a.E) mine += (rows_of(e, lo) + BM - 1) / BM;
+  int before = 0, top;
+  bool sorted = true;
+  int mine = count(0, top, sorted);
+  if (__ballot(!sorted) != 0) {
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(top, o);
+      if (lane >= o) top = max(top, v);
+    }
+    before = __shfl_up(top, 1);
+    if (lane == 0) before = 0;
+    mine = count(before, top, sorted);
   }
   int upto = mine;
 #pragma unroll
@@ -234,15 +259,15 @@ __device__ __forceinline__ GroupTile find_tile(const ExpertArgs& a, int cols, in
   GroupTile g;
   g.any = at < chunk && t < total;
   if (!g.any) return g;
-  // offsets that overlap can add up to more tiles than the launch has, or wrap
-  // the sum: then no expert may hold t, and the search ends at the last one
-  const unsigned long long past = __ballot((long)upto * cols > t);
-  const int owner = past != 0 ? __builtin_ctzll(past) : 63;
+  const int owner = __builtin_ctzll(__ballot((long)upto * cols > t));
   long left = t - (long)__builtin_amdgcn_readlane(upto - mine, owner) * cols;
+  int next = max(__builtin_amdgcn_readlane(before, owner), offset(owner * per));
   for (g.e = owner * per; g.e < a.E; ++g.e) {
-    g.len = rows_of(g.e, g.lo);
+    g.lo = next;
+    next = max(g.lo, offset(g.e + 1));
+    g.len = next - g.lo;
     const int mt = (g.len + BM - 1) / BM;
-    if (left >= 0 && left < (long)mt * cols) {
+    if (left < (long)mt * cols) {
       const int band = (int)(left / (kBand * cols)), in = (int)(left % (kBand * cols));
       const int high = min(kBand, mt - band * kBand);
       g.m0 = (band * kBand + in % high) * BM;
@@ -253,6 +278,17 @@ __device__ __forceinline__ GroupTile find_tile(const ExpertArgs& a, int cols, in
   }
   g.any = false;
   return g;
+}
+
+// first row of group e, M(e) as above
+__device__ __forceinline__ int group_start(const ExpertArgs& a, int e, int lane) {
+  const int own = clampi(a.offsets[e], 0, a.rows);
+  int most = own;
+#pragma unroll 4
+  for (int q = 0; q < e; q += 64) most = max(most, clampi(a.offsets[min(q + lane, e)], 0, a.rows));
+  if (__ballot(most > own) == 0) return own;
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o));
+  return __builtin_amdgcn_readfirstlane(most);
 }
 
 // an XCD's tiles of an expert in bwd_w
@@ -293,7 +329,8 @@ __global__ __launch_bounds__(64 * MW * NW, 2) void experts_kernel(ExpertArgs a) 
     g.m0 = (band * kBand + in % high) * BM;
     g.n0 = in / high % tiles_n * BN;
     g.part = in / high / tiles_n;
-    g.lo = clampi(a.offsets[g.e], 0, a.rows);
+    if (!a.overwrite && a.offsets[g.e + 1] <= a.offsets[g.e]) return;  // M(e) is no smaller
+    g.lo = group_start(a, g.e, lane);
     g.len = clampi(a.offsets[g.e + 1], g.lo, a.rows) - g.lo;
     if (g.len == 0 && !a.overwrite) return;
   } else {

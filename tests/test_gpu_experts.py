@@ -305,3 +305,53 @@ def test_repeats_streams_and_graphs(gpu):
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(outs[0], outs[2]))
             call(*outs[1])
+
+
+def _raised(off, rows):
+    return np.maximum.accumulate(np.clip(off, 0, rows))
+
+
+@pytest.mark.parametrize("name,i,o", [
+    ("back", 64, 128), ("back", 256, 384), ("many", 72, 64), ("most", 40, 136), ("large", 264, 264), ("first", 64, 64),
+    ("large", 1024, 2056)])
+def test_offsets_out_of_order_are_raised(gpu, name, i, o):
+    """Bitwise what the clamped offsets' running maximum gives: no row belongs to
+    two experts, and none that it gives to one is left out."""
+    import torch
+    from paper_2606_01143_amd import binding as B
+    _say(f"raised {name} {i} x {o}")
+    rng = np.random.default_rng(i)
+    noisy = lambda E, rows: np.sort(rng.integers(0, rows, E + 1)) + rng.integers(-rows // 3, 1, E + 1)
+    rows, off = {"back": (90, [0, 30, -5, 1 << 30]), "many": (500, noisy(200, 500)),
+                 "most": (700, [*noisy(1022, 700), -2147483648, 2147483647]), "first": (70, [50, 0, 20, 60, 60, 10]),
+                 "large": (2600, [0, 900, 400, 1500, 1400, -1, 2300, 2147483647, 0])}[name]
+    off = np.array(off)
+    want = _raised(off, rows)
+    s = _make([rows], i, o, tokens=60, seed=i)
+    E = len(off) - 1
+    g = torch.Generator(device="cuda").manual_seed(o)
+    w, w2 = (torch.randn(E, i, o, generator=g, device="cuda").bfloat16() for _ in range(2))
+    new = lambda *sh, dt=torch.bfloat16: torch.full(sh, 3.0, dtype=dt, device="cuda")
+    outs = []
+    for f in (want, off, off):
+        t = torch.from_numpy(f.astype(np.int32)).cuda()
+        r = [new(rows, o), new(rows, o), new(rows, i), new(rows, i), *(new(E, i, o, dt=torch.float32) for _ in range(4))]
+        B.experts_fwd(t, s["x"], w, r[0], w2=w2, y2=r[1], row_token=s["tok"])
+        B.experts_bwd_x(t, s["dy"], w, r[2], dy2=s["dy2"], w2=w2)
+        B.experts_bwd_x(t, s["dy"], w, r[3])
+        B.experts_bwd_w(t, s["x"], s["dy"], r[4], dy2=s["dy2"], dw2=r[5], row_token=s["tok"], overwrite=True)
+        xs = s["x"][s["tok"].long()]
+        B.experts_bwd_w(t, xs, s["dy"], r[6])
+        B.experts_bwd_w(t, xs, s["dy"], r[7], overwrite=True)
+        torch.cuda.synchronize()
+        outs.append(r)
+    for r in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], r))
+    # and the raised offsets are the groups of the formula
+    y, dw = outs[1][0], outs[1][4]
+    for e in range(E):
+        a, b = want[e], want[e + 1]
+        x, dy = s["x"].double()[s["tok"][a:b].long()], s["dy"][a:b].double()
+        _within(y[a:b], x @ w[e].double(), x.abs() @ w[e].double().abs(), i, HALF, f"y of expert {e}")
+        _within(dw[e], x.t() @ dy, x.abs().t() @ dy.abs(), b - a, 0.0, f"dw of expert {e}")
+    assert (y[:want[0]] == 3).all() and (y[want[-1]:] == 3).all()
