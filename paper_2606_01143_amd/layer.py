@@ -33,13 +33,20 @@ W_KEYS = ("wq", "wk", "wv", "wo", "wg", "wu", "wd")
 HEAD_GAINS = ("gq", "gk")
 
 
+def weight_keys(weights):
+    """The keys of a layer's weights: the seven, and the gains where it has them."""
+    gains = tuple(k for k in HEAD_GAINS if k in weights)
+    if len(gains) == 1:
+        raise ValueError("the gains of queries and keys go together")
+    return W_KEYS + gains
+
+
 class DecoderLayer:
     def __init__(self, inp: Dict, device="cuda:0"):
         shp = inp["shape"]
         dev = torch.device(device)
         up = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(device=dev, dtype=torch.bfloat16)
-        gains = tuple(k for k in HEAD_GAINS if k in inp["weights"])
-        self._setup(shp, {k: up(inp["weights"][k]) for k in W_KEYS + gains}, dev, None)
+        self._setup(shp, {k: up(inp["weights"][k]) for k in weight_keys(inp["weights"])}, dev, None, None)
         self.x_p = up(inp["x_p"])
         self.x_s = [up(x) for x in inp["x_s"]]
         self.dy_s = [up(x) for x in inp["dy_s"]]
@@ -49,22 +56,22 @@ class DecoderLayer:
             torch.zeros_like(self.x_p)
 
     @classmethod
-    def of_weights(cls, shape, weights: Dict[str, torch.Tensor], device, ws: Optional[torch.Tensor] = None):
+    def of_weights(cls, shape, weights: Dict[str, torch.Tensor], device, ws: Optional[torch.Tensor] = None,
+                   ws_heads: Optional[torch.Tensor] = None):
         """A layer of a stack: its bf16 weights on the device, its own gK/gV
-        cache; ``ws`` a workspace shared by the stack's layers."""
+        cache; ``ws`` (and ``ws_heads``, where layers normalise their heads)
+        workspaces shared by the stack's layers."""
         layer = cls.__new__(cls)
-        layer._setup(shape, weights, torch.device(device), ws)
+        layer._setup(shape, weights, torch.device(device), ws, ws_heads)
         return layer
 
-    def _setup(self, shp, weights, dev, ws):
+    def _setup(self, shp, weights, dev, ws, ws_heads):
         if shp.dtype != "bf16":
             raise ValueError("the layer path runs in bf16")
-        if ("gq" in weights) != ("gk" in weights):
-            raise ValueError("the gains of queries and keys go together")
         self.shape = shp
         self.dev = dev
         self.w = weights
-        self.head_norm = "gq" in weights
+        self.head_norm = "gq" in weight_keys(weights)
         hq, hkv, d, P = shp.num_q_heads, shp.num_kv_heads, shp.head_dim, shp.prefix_len
         self.dims = B.make_dims(hq, hkv, d, P, "bf16")
         self.gk = torch.zeros(P, hkv, d, dtype=torch.float32, device=self.dev)
@@ -72,10 +79,9 @@ class DecoderLayer:
         if ws is None:
             ws = torch.empty(self.workspace_bytes(shp), dtype=torch.uint8, device=self.dev)
         self.ws = ws
-        if self.head_norm:
-            longest = P + max(shp.suffix_lens, default=0)
-            self.ws_heads = torch.empty(B.head_norm_rope_bwd_workspace_size(longest, hq, hkv, d), dtype=torch.uint8,
-                                        device=self.dev)
+        if self.head_norm and ws_heads is None:
+            ws_heads = torch.empty(self.head_workspace_bytes(shp), dtype=torch.uint8, device=self.dev)
+        self.ws_heads = ws_heads
         self._cu = {}
         self._dense_dims = {}
 
@@ -85,6 +91,12 @@ class DecoderLayer:
         mx = max(shp.suffix_lens) if shp.n else 1
         return max(B.workspace_size(B.OP_PREFIX_BWD, dims), B.workspace_size(B.OP_SUFFIX_FWD, dims, 1, mx, mx),
                    B.workspace_size(B.OP_SUFFIX_BWD, dims, 1, mx, mx), 256)
+
+    @staticmethod
+    def head_workspace_bytes(shp) -> int:
+        """The per-head norm's backward, of a whole trajectory (the dense path's rows)."""
+        return B.head_norm_rope_bwd_workspace_size(shp.prefix_len + max(shp.suffix_lens, default=0), shp.num_q_heads,
+                                                   shp.num_kv_heads, shp.head_dim)
 
     # ---------------------------------------------------------- token-wise
     def _forward(self, x: torch.Tensor, pos0: int, attend) -> Dict[str, torch.Tensor]:

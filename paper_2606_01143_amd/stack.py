@@ -16,7 +16,8 @@ are every layer's prefix part plus its suffix parts (App. A.6).
 Per layer the schedule keeps a *hot* set resident through Phase B: the
 prefix K/V (after RoPE) that the suffixes attend to, and the cache.  The
 rest of what Phase A saves for Phase C is *dormant* during Phase B: the
-layer's input, both norms' outputs and statistics, the prefix queries,
+layer's input, both norms' outputs and statistics, the prefix queries (and,
+in a layer that normalises its heads, the queries and keys before that),
 attention output and LSE, the residual stream after attention and the MLP
 activations.  With ``offload=True`` each layer's dormant set is packed to
 pinned host memory right after its Phase A (asynchronously, on a copy
@@ -34,7 +35,7 @@ import numpy as np
 import torch
 
 from . import binding as B
-from .layer import DecoderLayer, W_KEYS
+from .layer import DecoderLayer, weight_keys
 
 
 # ---------------------------------------------------------------- host side
@@ -94,6 +95,11 @@ class HbmBudget:
 # what Phase A of a layer saves for its Phase C besides the hot prefix K/V
 # (the layer's prefix output is the next layer's input "x")
 _DORMANT = ("x", "n1", "r1", "q", "o", "lse", "h", "n2", "r2", "g", "u", "m")
+_DORMANT_HEADS = ("q0", "k0")  # of a layer that normalises its heads
+
+
+def _dormant_keys(layer):
+    return _DORMANT + (_DORMANT_HEADS if layer.head_norm else ())
 
 
 class DecoderStack:
@@ -113,7 +119,7 @@ class DecoderStack:
         if inp is not None:
             shape, layers = inp["shape"], len(inp["weights"])
             up = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(device=self.dev, dtype=bf)
-            weights = [{k: up(w[k]) for k in W_KEYS} for w in inp["weights"]]
+            weights = [{k: up(w[k]) for k in weight_keys(w)} for w in inp["weights"]]
             self.x_p = up(inp["x_p"])
             self.x_s = [up(x) for x in inp["x_s"]]
             self.dy_s = [up(x) for x in inp["dy_s"]]
@@ -138,17 +144,23 @@ class DecoderStack:
                     else torch.zeros_like(self.x_p))
         self.dy_p = dy_p
         self.ws = torch.empty(DecoderLayer.workspace_bytes(shape), dtype=torch.uint8, device=self.dev)
-        self.layers = [DecoderLayer.of_weights(shape, w, self.dev, self.ws) for w in weights]
+        self.ws_heads = None
+        if any("gq" in w for w in weights):
+            self.ws_heads = torch.empty(DecoderLayer.head_workspace_bytes(shape), dtype=torch.uint8, device=self.dev)
+        self.layers = [DecoderLayer.of_weights(shape, w, self.dev, self.ws, self.ws_heads) for w in weights]
         self.offload = offload
         self.budget = budget or HbmBudget()
         self.copy_stream = torch.cuda.Stream(self.dev) if offload else None
         P, hid, I = shape.prefix_len, shape.hidden, shape.intermediate
-        hq, d = shape.num_q_heads, shape.head_dim
-        # bytes of one layer's dormant set: bf16 rows of the hidden width
+        hq, hkv, d = shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+        # bytes of each layer's dormant set: bf16 rows of the hidden width
         # (x, n1, h, n2), the query width (q, o) and the MLP width (g, u, m),
-        # fp32 norm statistics (r1, r2) and LSE
-        self.layer_dormant_bytes = P * (2 * (4 * hid + 2 * hq * d + 3 * I) + 4 * (2 + hq))
-        self.dormant_bytes = self.layer_dormant_bytes * layers
+        # fp32 norm statistics (r1, r2) and LSE; where heads are normalised,
+        # bf16 queries and keys before it (q0, k0)
+        plain = P * (2 * (4 * hid + 2 * hq * d + 3 * I) + 4 * (2 + hq))
+        self.dormant_bytes_of = [plain + (P * 2 * (hq + hkv) * d if layer.head_norm else 0) for layer in self.layers]
+        self.layer_dormant_bytes = max(self.dormant_bytes_of, default=plain)  # the largest layer's
+        self.dormant_bytes = sum(self.dormant_bytes_of)
         self.pool = PinnedPool(int(self.dormant_bytes * pool_factor)) if offload else None
         self.stats = {"prefetched": 0, "demand_loaded": 0, "pool_fallbacks": 0}
         L = layers
@@ -167,7 +179,7 @@ class DecoderStack:
         cs.wait_event(done)
         c = self._saved[l]
         with torch.cuda.stream(cs):
-            for k in _DORMANT:
+            for k in _dormant_keys(self.layers[l]):
                 x = c[k]
                 h = self.pool.take(x.numel() * x.element_size()).view(x.dtype).view(x.shape)
                 h.copy_(x, non_blocking=True)
@@ -188,7 +200,7 @@ class DecoderStack:
         if not prefetch and self._packed[l] is not None:
             stream.wait_event(self._packed[l])
         with torch.cuda.stream(stream):
-            for k in _DORMANT:
+            for k in _dormant_keys(self.layers[l]):
                 h = self._host[l][k]
                 x = torch.empty(h.shape, dtype=h.dtype, device=self.dev)
                 x.copy_(h, non_blocking=True)
@@ -202,7 +214,7 @@ class DecoderStack:
     def _try_prefetch(self, l: int) -> None:
         if l < 0 or not self.offload or self._saved[l]["q"] is not None or self._ready[l] is not None:
             return
-        if self.budget.allows(self.layer_dormant_bytes):
+        if self.budget.allows(self.dormant_bytes_of[l]):
             self._restore(l, prefetch=True)
 
     def _ensure_resident(self, l: int) -> None:
@@ -212,7 +224,7 @@ class DecoderStack:
         elif self._ready[l] is not None:
             main = torch.cuda.current_stream(self.dev)
             main.wait_event(self._ready[l])
-            for k in _DORMANT:
+            for k in _dormant_keys(self.layers[l]):
                 c[k].record_stream(main)
             self._ready[l] = None
 
