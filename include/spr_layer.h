@@ -50,11 +50,11 @@ spr_status spr_rope_bwd(int32_t tokens, int32_t heads, int32_t head_dim, int32_t
  * SPR_BF16 or SPR_F32 for every tensor but the gain gradients.
  * * q [tokens, q_heads, d], k [tokens, kv_heads, d]: d contiguous, heads d
  *   apart, tokens q_stride / k_stride elements apart (at least a token's own
- *   heads), so both may be views of one fused projection; any element
- *   alignment, 16 bytes (and strides of as much, d a multiple of 16) being
- *   the fast one.  gain_q, gain_k [d].  yq, yk contiguous, out; they overlap
- *   nothing.  tokens * (q_heads + kv_heads), and a token's elements, are at most
- * 2^31 - 1. */
+ *   heads, at most 2^31 - 1), so both may be views of one fused projection;
+ *   any element alignment, 16 bytes (and strides of as much, d a multiple of
+ *   16) being the fast one.  gain_q, gain_k [d].  yq, yk contiguous, out; they
+ *   overlap nothing.  tokens * (q_heads + kv_heads), and a token's elements,
+ *   are at most 2^31 - 1. */
 spr_status spr_head_norm_rope_fwd(int32_t dtype, int32_t tokens, int32_t q_heads, int32_t kv_heads,
                                   int32_t head_dim, float eps, int32_t pos0, const int32_t* positions,
                                   double theta, const void* q, int64_t q_stride, const void* k,

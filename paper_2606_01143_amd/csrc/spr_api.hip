@@ -1521,9 +1521,13 @@ spr_status check_heads(int32_t dtype, int32_t tokens, int32_t hq, int32_t hkv, i
   return SPR_OK;
 }
 spr_status check_strides(std::initializer_list<Rows> all) {
-  for (const Rows& r : all)
-    if (r.stride < (int64_t)r.width || r.stride > (INT64_MAX >> 34))
+  for (const Rows& r : all) {
+    if (r.stride < (int64_t)r.width)
       return fail(SPR_ERR_INVALID_ARG, std::string(r.name) + ": a token's stride is at least its heads' elements");
+    // tokens are at most 2^30 (two rows of heads each): their bytes stay within 64 bits
+    if (r.stride > INT32_MAX)
+      return fail(SPR_ERR_INVALID_ARG, std::string(r.name) + ": a token's stride exceeds 2^31 - 1 elements");
+  }
   return SPR_OK;
 }
 HeadArgs head_args(int32_t tokens, int32_t hq, int32_t hkv, int32_t d, float eps, int32_t pos0,

@@ -247,3 +247,29 @@ def test_captured_and_on_another_stream(gpu):
             torch.cuda.synchronize()
             assert all(torch.equal(o[n], e[n]) for n in o if n != "ws")
             _run(ins[0], 5, 1e-6)
+
+
+@pytest.mark.parametrize("d,stride", [(128, (1 << 30) + 8), (72, (1 << 30) + 9)])
+def test_far_strides(gpu, d, stride):
+    """Three tokens more than 2^30 elements apart give what contiguous ones give."""
+    import torch
+    from paper_2606_01143_amd import binding as B
+    _say(f"stride {stride} d {d}")
+    i = _inputs(3, 4, 2, d, torch.bfloat16, seed=d)
+    want = _run(i, 9, 1e-6)
+    buf = torch.empty(2 * stride + 6 * d, dtype=torch.bfloat16, device="cuda")
+    view = lambda b, a, n: b[a * d:].as_strided((3, n, d), (stride, d, 1))
+    q, k = view(buf, 0, 4), view(buf, 4, 2)
+    q.copy_(i["q"])
+    k.copy_(i["k"])
+    yq, yk = torch.empty_like(i["dyq"]), torch.empty_like(i["dyk"])
+    B.head_norm_rope_fwd(q, k, i["gq"], i["gk"], yq, yk, 9, THETA)
+    grad = torch.empty_like(buf)
+    dq, dk = view(grad, 0, 4), view(grad, 4, 2)
+    dgq, dgk = (torch.empty(d, device="cuda") for _ in range(2))
+    ws = torch.empty(B.head_norm_rope_bwd_workspace_size(3, 4, 2, d), dtype=torch.uint8, device="cuda")
+    B.head_norm_rope_bwd(q, k, i["gq"], i["gk"], i["dyq"], i["dyk"], dq, dk, dgq, dgk, 9, THETA, overwrite=True, ws=ws)
+    got = dict(yq=yq, yk=yk, dq=dq, dk=dk, dgq=dgq, dgk=dgk)
+    if d == 128:  # the same kernel: both take 16-byte chunks
+        assert all(torch.equal(t, want[n]) for n, t in got.items())
+    _check(i, got, 9 + np.arange(3.0), 1e-6)

@@ -187,3 +187,16 @@ def test_embed_sizes_that_a_launch_holds():
     for fwd in (True, False):
         assert _embed(fwd, T=1 << 27, w=4096, ids=None) == "SPR_ERR_INVALID_ARG" and "ids" in B.last_error()
         assert _embed(fwd, T=(1 << 27) + 1, w=4096, ids=None) == "SPR_ERR_INVALID_ARG" and "2^39" in B.last_error()
+
+
+def test_heads_strides():
+    """Up to 2^31 - 1 elements, which a token's own heads may have; the refusal
+    names the limit that was passed."""
+    far = dict(q=A, k=A + (1 << 44), T=2, gq=None)  # the NULL gain is found behind the strides
+    most = 2147483647
+    assert _heads_fwd(**far, qs=most, ks=1 << 30) == "SPR_ERR_INVALID_ARG" and "gain_q" in B.last_error()
+    assert _heads_bwd(**far, qs=most, ks=1 << 30, dqs=1 << 29, dks=most) == "SPR_ERR_INVALID_ARG"
+    assert "gain_q" in B.last_error()
+    for kw in (dict(qs=most + 1), dict(ks=1 << 40)):
+        assert _heads_fwd(**{**far, **kw}) == "SPR_ERR_INVALID_ARG" and "exceeds 2^31 - 1" in B.last_error()
+    assert _heads_fwd(qs=255) == "SPR_ERR_INVALID_ARG" and "at least" in B.last_error()
