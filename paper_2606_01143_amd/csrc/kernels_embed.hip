@@ -129,6 +129,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_few_kernel(const int* __r
 // Whole call of width 1024, us, by counting / in radix passes: 4096 tokens 23 /
 // 31, 8192 31 / 39, 12000 46 / 44.  (Eight lanes a token: 32 and 51.)
 constexpr int kRankTokens = 8192, kRankLanes = 32, kRankThreads = 1024;
+static_assert(kRankTokens >= kSortSelfCount, "a sort in radix passes has its counts in a launch of their own");
 
 __global__ __launch_bounds__(kRankThreads) void embed_rank_kernel(const int* __restrict__ ids, int tokens, int vocab,
                                                                   int* __restrict__ keys_out,
@@ -317,7 +318,7 @@ int embed_span(long n, long slabs) {
   return len;
 }
 // workspace: two buffers of keys and tokens, the histograms, then the parts of
-// runs that cross spans (none where one span holds all tokens)
+// runs that cross spans (more than kFewTokens tokens are several spans)
 struct EmbedWs {
   size_t item, hist, head, tail, total;
 };
@@ -327,7 +328,7 @@ EmbedWs embed_ws(long n, long width) {
   w.item = ((size_t)n * 4 + 255) / 256 * 256;
   w.hist = 4 * w.item;
   w.head = w.hist + (sort_hist_bytes(n, 1 << kSortRadixBits) + 255) / 256 * 256;
-  const size_t part = n > len ? (size_t)((n + len - 1) / len) * width * 4 : 0;
+  const size_t part = (size_t)((n + len - 1) / len) * width * 4;
   w.tail = w.head + part;
   w.total = w.tail + part;
   return w;
@@ -390,7 +391,7 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
   for (int shift = 0, left = n <= kRankTokens ? 0 : sort_bits(vocab); left > 0; left -= kSortRadixBits, shift += kSortRadixBits) {
     const int bits = left < kSortRadixBits ? left : kSortRadixBits;
     const SortPass p = {k_in, n, per, vocab, shift, bits, 1 << bits, nb, hist};
-    if (sort_counts(n)) {
+    {
       ProfileScope ps("sort_count", st);
       hipLaunchKernelGGL(sort_count_kernel, dim3(nb), dim3(kSortThreads), 0, st, p);
     }
@@ -414,7 +415,7 @@ hipError_t launch_embed_bwd(int dtype, int tokens, int vocab, int width, float s
       hipLaunchKernelGGL(embed_runs_kernel<float>, grid, dim3(kEmbedThreads), 0, st, k_in, t_in, (const float*)dy,
                          dtable, head, tail, tokens, vocab, chunks, slabs, len, scale);
   }
-  if (n > len) {
+  {
     ProfileScope ps("embed_join", st);
     hipLaunchKernelGGL(embed_join_kernel, grid, dim3(kEmbedThreads), 0, st, k_in, dtable, head, tail, tokens, vocab,
                        chunks, slabs, len, scale);

@@ -649,7 +649,7 @@ hipError_t launch_tiles(const ExpertArgs& a, hipStream_t st) {
 // counted from the rows' average, a good half tile of padding per expert that has
 // rows; half a round is added for the last one where there are several.
 // Measured 256 / 128, us: 128 experts of 2048 x 768 top-8, forward, tokens 1024
-// 195 / 171, 2045 207 / 213, 4096 269 / 306, 8192 432 / 530; eight of 4096 x
+// 195 / 171, 2045 207 / 213 (128 is taken), 4096 269 / 306, 8192 432 / 530; eight of 4096 x
 // 1536 top-2, 300 tokens, forward 91 / 62, row gradients 74 / 60; 1000 tokens 97
 // / 85 and 86 / 118.
 bool small_tiles(const ExpertArgs& a, int cols_of_c, int parts) {
