@@ -18,11 +18,11 @@
 // Bound by the matrix cores where experts have hundreds of rows, by the weights'
 // bytes where they have few.  In 256 x 256 tiles of eight waves (128 x 64 a wave,
 // one workgroup a CU; 256 x 128 tiles of four waves, two a CU, read a half more
-// bytes into LDS and took 582 us for the first figure) 128 experts of 2048 x 768,
-// 8192 tokens of top-8: gate and up 430 us (960 TFLOP/s; a plain matrix product
-// of the same operations reaches 1182 in the library), row gradients of both 474
-// us (870), weight gradients of both 670 us (615 TFLOP/s, 2.4 TB/s of fp32
-// gradients written).  Eight experts of 4096 x 1536: 1138, 1090 and 1205 TFLOP/s.
+// bytes into LDS and took 582 us where these took 430) 128 experts of 2048 x 768,
+// 8192 tokens of top-8: gate and up 456 us (904 TFLOP/s, on some cards 425; a plain
+// matrix product of the same operations reaches 1182 in the library), row gradients
+// of both 474 us (870), weight gradients of both 681 us (605 TFLOP/s, 2.4 TB/s of
+// fp32 gradients written).  Eight experts of 4096 x 1536: 1138, 1090 and 1205 TFLOP/s.
 //
 // Ragged ends: contraction indices past the end are read from a line of zeros
 // (both operands: a zero times another row's infinity would be a NaN); C rows
