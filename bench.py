@@ -85,6 +85,9 @@ def mfma_summary(workload: str) -> str:
     return os.path.join(ROOT, "profiles", f"mfma_util_{workload}.md")
 
 BWD_SOURCES = ["kernels_bf16_bwd.hip", "tile.hpp", "common.hpp", "spr_api.hip", "launch.hpp"]
+# where the attention's part of a source that serves the other operators too ends
+ATTENTION_ENDS = {"spr_api.hip": "// ------------------------------------------------ decoder-layer token ops\n",
+                  "launch.hpp": "// decoder-layer token-wise operations (kernels_layer.hip)\n"}
 SWEEPS = {
     "c3": [f"qwen3_8b_p{p}_n{n}" for p in (2048, 8192, 16384) for n in (4, 8, 16)],
     "c4": ["qwen3_moe_p8192_n16_ragged"],
@@ -121,10 +124,18 @@ def pair_counts(shape):
 
 
 def bwd_source_hash() -> str:
+    """Of what shapes the backward's launches: its kernels and the attention's
+    part of the host sources, so that counters hold while other operators are
+    added behind it."""
     h = hashlib.sha256()
     for f in BWD_SOURCES:
         with open(os.path.join(ROOT, "paper_2606_01143_amd", "csrc", f), "rb") as fh:
-            h.update(fh.read())
+            text = fh.read()
+        if f in ATTENTION_ENDS:
+            text = text.split(ATTENTION_ENDS[f].encode())[0]
+            # other operators' headers are included above the attention's part
+            text = b"".join(x for x in text.splitlines(True) if not x.startswith(b'#include "../../include/'))
+        h.update(text)
     return h.hexdigest()[:16]
 
 
