@@ -262,7 +262,7 @@ class DecoderStack:
                                       self.ws)
 
                 c = layer._forward(x, P, suffix_attn)
-                x = c["y"]
+                x = c.pop("y")
                 acts.append(c)
             y_s.append(x)
             if i == len(self.x_s) - 1:
@@ -320,7 +320,7 @@ class DecoderStack:
                     B.prefix_fwd(dims, c["q"], c["k"], c["v"], c["o"], c["lse"])
 
                 c = layer._forward(x, 0, attn)
-                x = c["y"]
+                x = c.pop("y")
                 acts.append(c)
             g = torch.cat([dy_p, dy_s])
             for l in reversed(range(L)):
