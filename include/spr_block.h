@@ -98,6 +98,8 @@ spr_status spr_block_norm_bwd_workspace_size(int32_t rows, int32_t width, size_t
  * * g = x w_gate and u = x w_up are kept for the backward where g and u are not
  *   NULL: [rows, mid_width] bf16, or int8 with exponents where g_e and u_e are
  *   not NULL.
+ * * Sizes: as spr_experts.h's products, and no more tiles than one launch holds:
+ *   about 2^23 of 256 rows of an expert by 128 columns of m (256 in the backward).
  * The down product is spr_experts_fwd, or a BLAS product of a dense block. */
 enum { SPR_ACT_SILU = 0, SPR_ACT_GELU_TANH = 1 };
 spr_status spr_glu_fwd(int32_t act, int32_t n_experts, int32_t rows, int32_t in_width, int32_t mid_width,

@@ -206,7 +206,6 @@ hipError_t launch_split(const ExpertArgs& a, hipStream_t st) {
   const long some = a.E < a.rows ? a.E : a.rows;
   long grid = (long)((ncols + CN - 1) / CN) * ((a.rows + some * 31) / 32);
   grid = (grid + kXcds - 1) / kXcds * kXcds;
-  if (grid * (64L * W) > (long)UINT32_MAX) return hipErrorInvalidConfiguration;  // threads of a launch
   if (grid == 0) return hipSuccess;
   hipLaunchKernelGGL((glu_split_kernel<MODE, BN, STEP, W, RING>), dim3((unsigned)grid), dim3(64 * W), 0, st, a);
   return hipGetLastError();
@@ -235,25 +234,41 @@ hipError_t launch_split(const ExpertArgs& a, hipStream_t st) {
 // forms differ by the lines that they read whole and the CUs that they reach.)
 enum GluForm { k64x128, k128x128Deep, k128x128, k192x256, k256x256, kSplit, kSplitNarrow };
 struct GluCost {
-  int rows, cols, slots;                    // of a tile; cols of the result
+  int rows, cols, slots, threads;           // of a tile (cols of the result), the card, a workgroup
   double step, step_full, tile, tile_full;  // us: alone, and more where all slots are taken
 };
 constexpr int kGluForms = 6, kGluBwdForms = 7;
 constexpr GluCost kGluCost[kGluForms] = {
-    {64, 64, 512, 0.24, 0.57, 2.8, 0.1},  {128, 64, 256, 0.33, 0.31, 2.7, 1.0},  {128, 64, 512, 0.54, 0.75, 2.6, 0.6},
-    {192, 128, 256, 0.74, 0.72, 4.0, 0.}, {256, 128, 256, 0.75, 0.88, 5.0, 0.}, {32, 32, 512, 0.16, 0.33, 2.4, 0.}};
+    {64, 64, 512, 256, 0.24, 0.57, 2.8, 0.1},   {128, 64, 256, 256, 0.33, 0.31, 2.7, 1.0},
+    {128, 64, 512, 256, 0.54, 0.75, 2.6, 0.6},  {192, 128, 256, 512, 0.74, 0.72, 4.0, 0.},
+    {256, 128, 256, 512, 0.75, 0.88, 5.0, 0.},  {32, 32, 512, 256, 0.16, 0.33, 2.4, 0.}};
 constexpr GluCost kGluBwdCost[kGluBwdForms] = {
-    {64, 128, 512, 0.21, 0.62, 3.2, 2.2},   {128, 128, 256, 0.24, 0.47, 4.4, 3.0},  {128, 128, 512, 0.38, 0.94, 4.0, 5.9},
-    {192, 256, 256, 0.75, 0.92, 4.0, 11.0}, {256, 256, 256, 0.77, 1.21, 5.0, 14.9}, {32, 64, 512, 0.07, 0.27, 3.8, 0.},
-    {32, 32, 256, 0.05, 0.07, 2.8, 0.}};
+    {64, 128, 512, 256, 0.21, 0.62, 3.2, 2.2},   {128, 128, 256, 256, 0.24, 0.47, 4.4, 3.0},
+    {128, 128, 512, 256, 0.38, 0.94, 4.0, 5.9},  {192, 256, 256, 512, 0.75, 0.92, 4.0, 11.0},
+    {256, 256, 256, 512, 0.77, 1.21, 5.0, 14.9}, {32, 64, 512, 192, 0.07, 0.27, 3.8, 0.},
+    {32, 32, 256, 256, 0.05, 0.07, 2.8, 0.}};
+
+// Whether a launch, of at most 2^32 - 1 threads, holds a form's tiles: at most one
+// of rows that is not whole for every expert with rows, as many workgroups on every
+// XCD.  Where one form's do not fit, larger tiles' may.
+inline bool launches(const GluCost& c, int experts, long rows, long cols) {
+  const long some = std::min<long>(experts, rows);
+  const long groups = (cols + c.cols - 1) / c.cols * ((rows + some * (c.rows - 1)) / c.rows);
+  return (groups + 7) / 8 * 8 * c.threads <= (long)UINT32_MAX;
+}
+template <int FORMS>
+bool glu_fits(const GluCost (&cost)[FORMS], int experts, long rows, long cols) {
+  return std::any_of(cost, cost + FORMS, [&](const GluCost& c) { return launches(c, experts, rows, cols); });
+}
 
 template <int FORMS>
 int glu_form(const GluCost (&cost)[FORMS], int experts, long rows, long cols, long depth, double weight_mb) {
   const double some = (double)std::min<long>(experts, rows);
   int best = 0;
-  double least = 0.;
+  double least = -1.;
   for (int f = 0; f < FORMS; ++f) {
     const GluCost& c = cost[f];
+    if (!launches(c, experts, rows, cols)) continue;
     const double high = experts == 1 ? (double)((rows + c.rows - 1) / c.rows)
                                      : std::max(some, (double)rows / c.rows + 0.5 * some);
     const double x = high * (double)((cols + c.cols - 1) / c.cols) / c.slots, fill = std::min(x, 1.);
@@ -261,7 +276,7 @@ int glu_form(const GluCost (&cost)[FORMS], int experts, long rows, long cols, lo
     const double steps = (double)((depth + 63) / 64);
     const double bytes = some * weight_mb / (FORMS == kGluForms && f == kSplit ? 3.3 : 4.9);  // at TB/s
     const double t = std::max(rounds * (steps * (c.step + c.step_full * fill) + c.tile + c.tile_full * fill), bytes);
-    if (f == 0 || t < least) {
+    if (least < 0. || t < least) {
       best = f;
       least = t;
     }
@@ -271,6 +286,7 @@ int glu_form(const GluCost (&cost)[FORMS], int experts, long rows, long cols, lo
 
 template <int MODE>
 hipError_t launch_glu(const ExpertArgs& a, int form, hipStream_t st) {
+  static_assert(kXcds == 8, "launches() counts workgroups of eight XCDs");
   switch (form) {
     case k64x128: return launch_tiles<MODE, 64, 128, 2, 2, 64, 3>(a, st);
     case k128x128Deep: return launch_tiles<MODE, 128, 128, 2, 2, 64, 4>(a, st);
@@ -283,6 +299,9 @@ hipError_t launch_glu(const ExpertArgs& a, int form, hipStream_t st) {
 }
 
 }  // namespace
+
+bool glu_fwd_fits(int experts, int rows, int mid_width) { return glu_fits(kGluCost, experts, rows, mid_width); }
+bool glu_bwd_fits(int experts, int rows, int mid_width) { return glu_fits(kGluBwdCost, experts, rows, mid_width); }
 
 hipError_t launch_glu_fwd(const ExpertArgs& a, hipStream_t st) {
   ProfileScope ps("glu_fwd", st);

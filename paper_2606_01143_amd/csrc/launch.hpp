@@ -249,7 +249,10 @@ hipError_t launch_experts_fwd(const ExpertArgs& a, hipStream_t st);
 hipError_t launch_experts_bwd_x(const ExpertArgs& a, hipStream_t st);
 hipError_t launch_experts_bwd_w(const ExpertArgs& a, hipStream_t st);
 
-// gated feed-forward (kernels_glu.hip)
+// gated feed-forward (kernels_glu.hip); whether a launch holds the tiles of any of its
+// forms, which the launches take for granted
+bool glu_fwd_fits(int experts, int rows, int mid_width);
+bool glu_bwd_fits(int experts, int rows, int mid_width);
 hipError_t launch_glu_fwd(const ExpertArgs& a, hipStream_t st);
 hipError_t launch_glu_bwd(const ExpertArgs& a, hipStream_t st);
 

@@ -1976,6 +1976,10 @@ spr_status check_act(int32_t act) {
     return fail(SPR_ERR_UNSUPPORTED, "act must be SPR_ACT_SILU or SPR_ACT_GELU_TANH");
   return SPR_OK;
 }
+spr_status check_glu_launch(bool fits) {
+  if (!fits) return fail(SPR_ERR_INVALID_ARG, "rows and mid_width need more threads than a launch has");
+  return SPR_OK;
+}
 spr_status check_kept_pair(const void* g, const void* g_e, const void* u, const void* u_e) {
   spr_status st = check_pair("g and u", g, u);
   if (st != SPR_OK) return st;
@@ -2131,6 +2135,7 @@ spr_status spr_glu_fwd(int32_t act, int32_t n_experts, int32_t rows, int32_t in_
   if (st != SPR_OK) return st;
   if ((st = check_products(n_experts, rows, in_width, mid_width, row_token != nullptr, x_rows)) != SPR_OK) return st;
   if (rows == 0) return ok();
+  if ((st = check_glu_launch(glu_fwd_fits(n_experts, rows, mid_width))) != SPR_OK) return st;
   if ((st = check_kept_pair(g, g_e, u, u_e)) != SPR_OK) return st;
   const size_t wb = (size_t)n_experts * in_width * mid_width * 2, n = (size_t)rows * mid_width;
   const Buf bufs[] = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", n_experts > 1, 4},
@@ -2162,6 +2167,7 @@ spr_status spr_glu_bwd(int32_t act, int32_t n_experts, int32_t rows, int32_t mid
   if (st != SPR_OK) return st;
   if ((st = check_products(n_experts, rows, mid_width, out_width, false, rows)) != SPR_OK) return st;
   if (rows == 0) return ok();
+  if ((st = check_glu_launch(glu_bwd_fits(n_experts, rows, mid_width))) != SPR_OK) return st;
   if ((st = check_kept_pair(g, g_e, u, u_e)) != SPR_OK) return st;
   const size_t n = (size_t)rows * mid_width;
   const Buf bufs[] = {{offsets, ((size_t)n_experts + 1) * 4, "offsets", n_experts > 1, 4},
