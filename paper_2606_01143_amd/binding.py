@@ -636,8 +636,8 @@ def experts_plan(n_experts, experts, offsets, row_token, pos, ws=None, stream=No
 
 
 def _groups(offsets, w, name="w"):
-    """n_experts and the shape of a weight [E, in, out], or of one dense
-    block's [in, out], which goes without offsets; and a view with E in front."""
+    """(E, in, out) of a weight [E, in, out], or with E = 1 of one dense block's
+    [in, out], which goes without offsets."""
     if w.dim() == 2:
         if offsets is not None:
             raise ValueError(f"{name} [in, out] is one dense block's: no offsets")

@@ -2,12 +2,17 @@
 // residual in one pass, and activations kept in 8 bits.
 //   p = f r_f g_post,  h = a x + b gate p,  n = h r_h g_pre
 // Both directions read each tensor once and write each once: HBM bound.  A row
-// stays in its workgroup's registers between its sums and its outputs; one row a
-// workgroup of a thread per eight values (two chunks a thread past 8192 columns).
+// stays in its threads' registers between its sums and its outputs, eight values a
+// thread (two chunks of eight past 8192 columns).  The forward has a row a workgroup;
+// a workgroup of the backward holds as many rows at once as fill 512 threads.
 // Measured, 28672 rows of 4096 bf16: residual, norm and an 8-bit copy 184 us (5.8
-// TB/s); norms on both sides and a gate 180 us, backward 272 us (5.2 TB/s); 2048
+// TB/s); norms on both sides and a gate 181 us, backward 277 us (5.1 TB/s); 2048
 // columns from 8 bits, 17543 rows, backward 80-85 us (4.4 TB/s; half its
 // instructions turn bytes into fp32) and 5 us for the columns' sums.
+// 1024 threads leave a thread 128 registers, and the backward's column sums spill some
+// there: 34 of fp32 rows from 4104 columns (4096 rows of 8192: 189 us where the bytes
+// take 164), 103 of fp32 and 6 of bf16 rows past 8192 columns (4096 rows of 8200: 396 and
+// 129 us, 164 and 82).
 #include "act8.hpp"
 #include "launch.hpp"
 
@@ -100,7 +105,6 @@ struct RowSums {
 };
 
 // a thread's eight values to 8 bits; every lane of its quad takes part
-template <typename T>
 __device__ __forceinline__ void pack8(const float (&v)[8], bool inside, void* q, uint8_t* e, size_t at, size_t block,
                                       bool first) {
   unsigned most = 0;
@@ -114,7 +118,7 @@ __device__ __forceinline__ void pack8(const float (&v)[8], bool inside, void* q,
 }  // namespace
 
 // ---------------------------------------------------------- block norm
-// A row a workgroup of TPR threads, CH chunks of eight values a thread.
+// Forward: a row a workgroup of TPR threads, CH chunks of eight values a thread.
 template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(TPR) void block_norm_fwd_kernel(BlockNormArgs a) {
   __shared__ float buf[2][TPR / 64][1];
@@ -158,7 +162,7 @@ __global__ __launch_bounds__(TPR) void block_norm_fwd_kernel(BlockNormArgs a) {
         const int ch = threadIdx.x + c * TPR;
         float v[8], g[8];
         f[c].values(v, false);
-        if (a.f8 != nullptr) pack8<T>(v, ch < chunks, a.f8, a.f_e, at + 8 * ch, block + ch / 4, ch % 4 == 0);
+        if (a.f8 != nullptr) pack8(v, ch < chunks, a.f8, a.f_e, at + 8 * ch, block + ch / 4, ch % 4 == 0);
         if (a.rstd_f != nullptr) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] *= r;
@@ -212,7 +216,7 @@ __global__ __launch_bounds__(TPR) void block_norm_fwd_kernel(BlockNormArgs a) {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int ch = threadIdx.x + c * TPR;
-        pack8<T>(h[c], ch < chunks, a.h8, a.h_e, at + 8 * ch, block + ch / 4, ch % 4 == 0);
+        pack8(h[c], ch < chunks, a.h8, a.h_e, at + 8 * ch, block + ch / 4, ch % 4 == 0);
       }
   }
 }
@@ -251,7 +255,8 @@ __global__ __launch_bounds__(TPR* ROWS) void block_norm_bwd_kernel(BlockNormArgs
   static_assert(!IN_LDS || ROWS == 1, "sums in LDS are of one row at a time");
   __shared__ f32x4 joined[ROWS > 1 || IN_LDS ? 4 * CH * TPR : 1];
   RowSums<TPR, 3, ROWS> sum{buf};
-  const int thread = threadIdx.x % TPR, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);  // a wave's rows are one group's
+  // (a wave's row is one group's: its place in memory stays in scalar registers)
+  const int thread = threadIdx.x % TPR, group = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   const int chunks = a.width / 8, blocks = (a.width + 31) / 32;
   const bool pre = a.dn != nullptr, post = a.rstd_f != nullptr, branch = a.f != nullptr, sums = needs_sums(a);
   const bool h8 = a.h_e != nullptr, f8 = a.f_e != nullptr, token_gate = a.gate_stride != 0;
@@ -478,7 +483,7 @@ __global__ __launch_bounds__(1024) void block_norm_sums_kernel(BlockNormArgs a, 
 
 namespace {
 
-// f<TPR, CH> of the least threads that hold a row in two chunks each at most
+// f<TPR, CH> of the least threads that hold a row in one chunk each, or 1024 of two
 template <typename F>
 hipError_t by_width(int width, F f) {
   const int chunks = width / 8;

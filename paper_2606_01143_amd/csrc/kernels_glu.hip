@@ -4,12 +4,12 @@
 // The tiles are experts.hpp's; this file holds the launches and their choice.
 //
 // Bound by the matrix cores where there are hundreds of rows, by the weights' bytes
-// where there are few.  28672 rows of 4096 x 14336: m alone 5010 us (1345 TFLOP/s; the
-// library's product of these sizes reaches 1302), m with g and u in 8 bits 5340 us,
-// backward from 8 bits 3170 us (1063 TFLOP/s: 25 us of a tile's 130 read g and u and
+// where there are few.  28672 rows of 4096 x 14336: m alone 5060 us (1331 TFLOP/s; the
+// library's product of these sizes reaches 1302), m with g and u in 8 bits 5370 us,
+// backward from 8 bits 3115 us (1081 TFLOP/s: 25 us of a tile's 130 read g and u and
 // write dg, du and m).  Four rows of it forward 47 us (5.0 TB/s of weights).
-// 128 experts of 2048 x 768, 8192 tokens of top-8: forward with bf16 g and u 455 us,
-// backward 329 us (3.9 TB/s).
+// 128 experts of 2048 x 768, 8192 tokens of top-8: forward with bf16 g and u 460 us,
+// backward 335 us (3.8 TB/s).
 #include <algorithm>
 
 #include "experts.hpp"
@@ -219,17 +219,22 @@ hipError_t launch_split(const ExpertArgs& a, hipStream_t st) {
 // one.  Where the weights are all there is to read their bytes count: the split
 // form of glu reads half a line of either weight at a time.
 // The constants (us) were fitted to one half of 529 sizes drawn from 1 to 28672
-// tokens, widths of 128 to 14336 and 1 to 128 experts; on the other half the form
-// taken is 2.0% (glu) and 2.2% (glu_bwd) slower than the best of all that were
-// timed.  Measured at 4096 x 14336, us for 4, 64, 128, 512, 1299, 28672 tokens:
-//   glu      64 x 128 47 51 85 199 - -, 128 x 128 deep 50 53 57 170 - -, 128 x 128 71
-//            72 73 160 379 6870, 192 x 256 93 93 95 176 355 6270, 256 x 256 94 93 98
-//            111 317 5520, split 71 104 165 511 - -
-//   glu_bwd  64 x 128 36 41 42 110 233 5030, 128 x 128 deep 36 41 53 98 220 4440, 128 x
-//            128 59 61 66 92 219 3860, 192 x 256 75 79 88 102 200 3500, 256 x 256 77 81
-//            90 117 229 3210
-// and the split forms against the best other: glu 4 tokens of 4624 x 128 10.7 / 20.9,
-// 253 of 1560 x 336 10.9 / 14.8; glu_bwd 339 of 3784 x 336 narrow 13, wide 15, other 30.
+// tokens, widths of 128 to 14336 and 1 to 128 experts, before the backward's stores
+// went past the caches.  Timed again on these kernels, the form taken is on the other
+// half 1.3% (glu) and 1.6% (glu_bwd) slower than the best of them on average.  The worst of
+// all 529 are 41% (glu, 60 experts of 3888 x 352, 29 tokens) and 27% (glu_bwd, 128 rows of
+// 4096 x 14336, as the table shows; 96 rows take 48 us where 64 x 128 takes 40).
+// Measured at 4096 x 14336, us for 4, 64, 128, 256, 512, 1299, 28672 tokens, glu keeping
+// neither g nor u, glu_bwd from 8 bits and with m, the form taken marked *:
+//   glu      64 x 128 48* 52* 85 118 199 435 9170, 128 x 128 deep 51 53 58* 95 169 380
+//            7670, 128 x 128 72 71 74 94 161 348 6410, 192 x 256 93 93 95 96 177 322 5730,
+//            256 x 256 94 94 97 102* 109* 297* 5060*, split 71 104 165 274 515 1085 -
+//   glu_bwd  64 x 128 35 40 42 65 113 234 4260, 128 x 128 deep 35 40 53* 55* 101 224 4220,
+//            128 x 128 58 61 66 69 93* 215 3730, 192 x 256 74 77 85 91 106 203* 3150, 256 x
+//            256 77 81 89 113 122 228 3115*, split 25* 36* 56 97 172 380 -, split narrow 27
+//            50 80 151 293 611 -
+// and the split forms against the best other: glu 4 tokens of 4624 x 128 10.5 / 22.0,
+// 253 of 1560 x 336 10.8 / 13.9; glu_bwd 339 of 3784 x 336 narrow 13, wide 18, other 31.
 // (A CU takes in about 43 KB a us, with 48 KB on their way as with 96: the split
 // forms differ by the lines that they read whole and the CUs that they reach.)
 enum GluForm { k64x128, k128x128Deep, k128x128, k192x256, k256x256, kSplit, kSplitNarrow };
