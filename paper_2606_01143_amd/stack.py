@@ -20,9 +20,10 @@ layer's input, both norms' outputs and statistics, the prefix queries (and,
 in a layer that normalises its heads, the queries and keys before that),
 attention output and LSE, the residual stream after attention and the MLP
 activations.  With ``saved="int8"`` the layers keep their input, the
-residual stream and the gate and up projections in 8 bits and form the
-rest again: less than half the bytes, of which Phase C's gradients carry the
-rounding.  With ``offload=True`` each layer's dormant set is packed to
+residual stream and the gate and up projections in 8 bits, of the prefix and
+of a suffix alike, and form the rest again: less than half the bytes, whose
+rounding the gradients of Phases B and C carry.  With ``offload=True`` each
+layer's dormant set is packed to
 pinned host memory right after its Phase A (asynchronously, on a copy
 stream) and restored for its Phase C: prefetched one layer ahead when an
 HBM budget check allows, demand-loaded otherwise.  That turns the dormant
